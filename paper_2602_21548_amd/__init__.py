@@ -16,12 +16,18 @@ _EXPORTS = (
     "kvl_unpack_layer_noalloc", "KVL_NOALLOC_MAX_UNITS",
     "kvl_ceiling_kernel", "KVL_CEILING_COPY", "KVL_CEILING_READ", "KVL_CEILING_WRITE",
 )
-__all__ = list(_EXPORTS)
+# attention over the loaded cache (include/kvl_attn.h)
+_ATTN_EXPORTS = (
+    "AttnPlan", "make_attn_layout", "kvl_attn_plan", "kvl_append_layer", "kvl_attn_layer",
+    "KVL_BF16", "KVL_F16", "KVL_E4M3", "KVL_ROPE_HALVES", "KVL_ROPE_NEIGHBOURS",
+)
+__all__ = list(_EXPORTS + _ATTN_EXPORTS)
 
 
 def __getattr__(name):
-    if name in _EXPORTS:
+    if name in __all__:
         # found here from now on: coming by this way took 3.6 us of every call
-        value = globals()[name] = getattr(importlib.import_module(".binding", __name__), name)
+        module = ".binding" if name in _EXPORTS else ".attn"
+        value = globals()[name] = getattr(importlib.import_module(module, __name__), name)
         return value
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -1,0 +1,694 @@
+// Attention over a paged cache: kernels.
+//
+// For a query q and the keys t that it sees, with c = scale * log2(e):
+//   m = max_t c <q, K_t>,  l = sum_t 2^(c <q, K_t> - m),  out = sum_t 2^(c <q, K_t> - m) V_t / l,  lse = ln 2 (m + log2 l),
+// in one pass over the keys: m, l and the unnormalised output are kept for the keys so far, and what is there is multiplied by
+// 2^(m - m') where a tile raises m to m'.  Results over different keys are joined by the same rule.
+//
+// The query heads that share a cache head are rows of one product: row = new token * group + head in group.
+//
+// Both kernels compute the scores' transpose, keys by rows of queries, S^T = K Q^T, and the outputs', O^T = V^T P^T.  In the
+// registers that the first product leaves, a lane holds one query row's scores, so m and l need no exchange but between the two or
+// four lanes that share a row; and what a lane holds of P^T is what the second product wants from it, if the keys of its contraction
+// are taken in the order in which they lie there.  V^T is read in that order, by the transposing reads of the LDS.
+#pragma once
+
+#include "kvl_attn_internal.h"
+#include "kvl_attn_types.h"
+
+namespace kvl {
+
+struct AttnArgs {
+    const AttnItem *items;
+    const int32_t *tables;
+    const char *k, *v;
+    const float *scale_k, *scale_v;
+    const char *q;
+    char *out;
+    float *lse;
+    float *workspace;
+    uint64_t q_stride, out_stride;      // elements
+    uint64_t div_mul;
+    uint32_t div_shift, block_tokens;
+    uint32_t kv_heads, group;
+    uint32_t window, sinks;             // window: 2^31 where there is none
+    float c;                            // scale * log2(e)
+};
+
+constexpr float kLowestScale = 0x1p-32f, kHighestScale = 0x1p63f;
+// Weights of fp16 are 2^8 times those of the formula: what is small beside the largest stays above fp16's least normal for longer.
+template <typename T>
+constexpr float kLift = 0.f;
+template <>
+constexpr float kLift<F16> = 8.f;
+
+typedef __attribute__((address_space(3))) char *lds_ptr;
+
+// 4 elements of a column out of the 16-lane group's 4 rows of 16: lane i of the group names 8 bytes, row i / 4, and gets column i.
+__device__ __forceinline__ u32x2 read_columns16(const char *at) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4 *ptr;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)(const_cast<char *>(at))));
+}
+// The same of bytes: 8 rows of 16, row i / 2.
+__device__ __forceinline__ u32x2 read_columns8(const char *at) {
+    typedef __attribute__((address_space(3))) i32x2 *ptr;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((ptr)(const_cast<char *>(at))));
+}
+
+// Where a key lies, and what its codes are multiplied by.
+struct KeyPlace {
+    uint32_t row;
+    float scale_k, scale_v;
+};
+template <bool E4M3>
+__device__ __forceinline__ KeyPlace find_key(const AttnArgs &a, const AttnItem &it, uint32_t head, uint32_t place) {
+    const uint32_t v = min(place, it.end - 1), t = v < it.sinks ? v : v + it.gap;
+    const uint32_t b = (uint32_t)((t * a.div_mul) >> a.div_shift);
+    const uint32_t id = (uint32_t)a.tables[it.table + b];
+    KeyPlace k;
+    k.row = id * a.block_tokens + (t - b * a.block_tokens);
+    if (E4M3) {
+        const uint64_t at = (uint64_t)id * a.kv_heads + head;
+        k.scale_k = fminf(fmaxf(a.scale_k[at], kLowestScale), kHighestScale);
+        k.scale_v = fminf(fmaxf(a.scale_v[at], kLowestScale), kHighestScale);
+    }
+    return k;
+}
+
+__device__ __forceinline__ bool sees(const AttnArgs &a, uint32_t position, uint32_t t) {
+    return t <= position && (t + a.window > position || t < a.sinks);
+}
+
+// Whether every query at positions [p0, p1] sees every key at places [v0, v1].
+__device__ __forceinline__ bool all_seen(const AttnArgs &a, const AttnItem &it, uint32_t v0, uint32_t v1, uint32_t p0, uint32_t p1) {
+    const uint32_t t0 = v0 < it.sinks ? v0 : v0 + it.gap, t1 = v1 < it.sinks ? v1 : v1 + it.gap;
+    return v1 < it.end && t1 <= p0 && (t0 + a.window > p1 || t1 < a.sinks);
+}
+
+// Whether some of the elements in a word, two of T or four codes, are infinite or NaN; and the word with zeros for them.
+template <typename T, bool E4M3>
+__device__ __forceinline__ bool odd_word(uint32_t w) {
+    if (E4M3) return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+    return (w & T::kExponent) == T::kExponent || ((w >> 16) & T::kExponent) == T::kExponent;
+}
+template <typename T, bool E4M3>
+__device__ __forceinline__ uint32_t plain_word(uint32_t w) {
+    if (E4M3) {
+        for (int i = 0; i < 32; i += 8)
+            if (((w >> i) & 0x7fu) == 0x7fu) w &= ~(0xffu << i);
+        return w;
+    }
+    for (int i = 0; i < 32; i += 16)
+        if (((w >> i) & T::kExponent) == T::kExponent) w &= ~(0xffffu << i);
+    return w;
+}
+template <typename T, bool E4M3, int N>
+__device__ __forceinline__ bool odd_pieces(const u32x4 (&x)[N]) {
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) odd = odd || odd_word<T, E4M3>(x[i][j]);
+    return odd;
+}
+template <typename T, bool E4M3, int N>
+__device__ __forceinline__ void make_plain(u32x4 (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[i][j] = plain_word<T, E4M3>(x[i][j]);
+}
+
+// The infinities and NaN among 4 values of row `row` from `dim` on, zeros for the rest.
+template <typename T, bool E4M3, int D>
+__device__ __forceinline__ f32x4 odd_values(const AttnArgs &a, uint32_t head, uint32_t row, uint32_t dim) {
+    const char *at = a.v + (((uint64_t)row * a.kv_heads + head) * D + dim) * (E4M3 ? 1 : 2);
+    f32x2 x, y;
+    if (E4M3) {
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(at);
+        x = widen_codes<0>(w);
+        y = widen_codes<1>(w);
+    } else {
+        const u32x2 w = *reinterpret_cast<const u32x2 *>(at);
+        x = T::widen(w[0]);
+        y = T::widen(w[1]);
+    }
+    f32x4 e{x[0], x[1], y[0], y[1]};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (fabsf(e[i]) < __builtin_inff()) e[i] = 0.f;
+    return e;
+}
+
+// 2^(m - to), where neither may be there yet (-inf)
+__device__ __forceinline__ float factor(float m, float to) { return m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - to); }
+
+// The output of one row: its sum, maximum and E unnormalised elements from `dim` on.
+template <typename T, int E>
+__device__ __forceinline__ void write_row(const AttnArgs &a, uint32_t token0, uint32_t row, uint32_t head, uint32_t dim, int head_dim, float l, const float (&o)[E]) {
+    const uint32_t token = token0 + row / a.group, h = head * a.group + row % a.group;
+    const float over = l == 0.f ? 0.f : 1.f / l;
+    uint32_t w[E / 2];
+#pragma unroll
+    for (int i = 0; i < E; i += 2) w[i / 2] = narrow<T>(o[i] * over, o[i + 1] * over);
+    char *to = a.out + 2 * (token * a.out_stride + (uint64_t)h * head_dim + dim);
+    __builtin_memcpy(__builtin_assume_aligned(to, 2 * E), w, 2 * E);
+}
+template <typename T>
+__device__ __forceinline__ void write_lse(const AttnArgs &a, uint32_t token0, uint32_t row, uint32_t head, float m, float l) {
+    if (!a.lse) return;
+    const uint64_t token = token0 + row / a.group, h = head * a.group + row % a.group;
+    a.lse[token * a.kv_heads * a.group + h] = l == 0.f ? -__builtin_inff() : 0.69314718055994531f * (m - kLift<T> + __log2f(l));
+}
+
+// Few rows -------------------------------------------------------------------------------------------------------------------------
+//
+// Up to 16 * RT rows against pieces of their keys.  The keys' and values' bytes bound it: each is read once, by one wavefront, and used
+// for all rows.  The wavefronts of a workgroup take tiles of keys in turn, each with its own maximum, sum and outputs, without a
+// barrier until the end, so that at any time all but the tile in work is on its way; then they are joined in the LDS.  K goes from memory
+// to the registers of the matrix instructions as it lies: lane (n, g) has key n's elements of four-lane group g, and the queries are laid out
+// to match.  V goes through the wavefront's own part of the LDS, which turns it.  8-bit codes become T there and here, exactly; their
+// scales multiply scores (K) and join the exponent (V: with x = c s_k <q, K_t> + log2 s_v, 2^(x - m) multiplies the codes, and 2^(x - m) / s_v
+// is the term of l), in 32 bits, whatever T is.
+template <typename T, bool E4M3, int D, int RT>
+__global__ void __launch_bounds__(256) kvl_attn_few_kernel(const AttnArgs a) {
+    constexpr int KT = few_rows_tile(E4M3, D), NB = KT / 16;        // keys of a tile, blocks of 16
+    constexpr int RB = D * (E4M3 ? 1 : 2);                          // bytes of a row
+    constexpr int PR = RB / 16;                                     // pieces of 16 bytes in it
+    constexpr int VP = KT * PR / 64;                                // a lane's pieces of V
+    constexpr int KP = RB / 64;                                     // a lane's pieces of K for each block
+    constexpr int CH = D / 32, DC = D / 16;                         // steps of the first product; blocks of the output
+    constexpr int kSwizzle = DC - 1;                                // rows of V are turned by their number, for the LDS banks' sake
+    constexpr int kWaveBytes = KT * RB + (E4M3 ? KT * 12 : 0);
+    constexpr int OS = D + 4;                                       // floats of an output row in the LDS
+    constexpr int kBytes = 4 * (kWaveBytes > 16 * OS * 4 ? kWaveBytes : 16 * OS * 4);
+    __shared__ __attribute__((aligned(16))) char lds[kBytes];
+    __shared__ f32x2 state[4][RT * 16];
+    typedef typename T::x8 x8;
+
+    const AttnItem it = a.items[blockIdx.x / a.kv_heads];
+    const uint32_t head = blockIdx.x % a.kv_heads;
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 16, g = lane / 16;
+    char *mine = lds + wave * kWaveBytes;
+    float *key_c = reinterpret_cast<float *>(mine + KT * RB), *key_log = key_c + KT, *key_over = key_log + KT;
+    const uint64_t row_pitch = (uint64_t)a.kv_heads * RB;
+    const char *k_head = a.k + head * RB, *v_head = a.v + head * RB;
+
+    x8 q[RT][CH];
+    uint32_t position[RT];
+    const uint32_t p0 = it.hit + it.first_row / a.group, p1 = it.hit + (it.first_row + it.n_rows - 1) / a.group;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const uint32_t i = min(r * 16 + n, it.n_rows - 1), row = it.first_row + i, token = row / a.group;
+        position[r] = it.hit + token;
+        const char *from = a.q + 2 * ((it.token0 + token) * a.q_stride + (head * a.group + row % a.group) * D);
+#pragma unroll
+        for (int s = 0; s < CH; ++s) {
+            const uint32_t dim = E4M3 ? (g + 4 * (s / 2)) * 16 + s % 2 * 8 : s * 32 + g * 8;
+            q[r][s] = *reinterpret_cast<const x8 *>(from + 2 * dim);
+        }
+    }
+    f32x4 o[RT][DC];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        m[r] = -__builtin_inff();
+        l[r] = 0;
+#pragma unroll
+        for (int d = 0; d < DC; ++d) o[r][d] = f32x4{0, 0, 0, 0};
+    }
+
+    u32x4 kr[NB][KP], vr[VP];
+    auto fetch = [&](const KeyPlace &at) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const char *from = k_head + __shfl(at.row, 16 * b + n) * row_pitch + g * 16;
+#pragma unroll
+            for (int i = 0; i < KP; ++i) kr[b][i] = *reinterpret_cast<const u32x4 *>(from + 64 * i);
+        }
+#pragma unroll
+        for (int i = 0; i < VP; ++i) vr[i] = *reinterpret_cast<const u32x4 *>(v_head + __shfl(at.row, (i * 64 + lane) / PR) * row_pitch + lane % PR * 16);
+    };
+
+    const uint32_t tiles = (it.end - it.begin + KT - 1) / KT;
+    KeyPlace at{}, next{};
+    if (wave < tiles) {
+        at = find_key<E4M3>(a, it, head, it.begin + wave * KT + lane % KT);
+        fetch(at);
+        next = find_key<E4M3>(a, it, head, it.begin + (wave + 4) * KT + lane % KT);
+    }
+    for (uint32_t tile = wave; tile < tiles; tile += 4) {
+        const uint32_t v0 = it.begin + tile * KT;
+        const bool whole = all_seen(a, it, v0, v0 + KT - 1, p0, p1);
+        // Values that only some of the rows see must not reach the others: 0 * inf is NaN.  Infinities and NaN of such a tile are added
+        // apart, to the rows that see them.
+        const bool odd = !whole && __any(odd_pieces<T, E4M3>(vr));
+        if (odd) make_plain<T, E4M3>(vr);
+#pragma unroll
+        for (int i = 0; i < VP; ++i) {
+            const uint32_t row = (i * 64 + lane) / PR, s = lane % PR;
+            const uint32_t to = E4M3 ? row * RB + ((s ^ (row & kSwizzle)) << 4) : row * RB + (((s >> 1) ^ (row & kSwizzle)) << 5) + ((s & 1) << 4);
+            *reinterpret_cast<u32x4 *>(mine + to) = vr[i];
+        }
+        if (E4M3) {
+            if (lane < KT) {
+                key_c[lane] = a.c * at.scale_k;
+                key_log[lane] = __log2f(at.scale_v);
+                key_over[lane] = 1.f / at.scale_v;
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+        // scores: lane (n, g) gets row n's of keys 16 b + 4 g + i
+        f32x4 s[RT][NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) s[r][b] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                x8 k;
+                if (E4M3) {
+                    const uint32_t w0 = kr[b][j / 2][j % 2 * 2], w1 = kr[b][j / 2][j % 2 * 2 + 1];
+                    const u32x4 w{T::template from_codes<false>(w0, 1.f), T::template from_codes<true>(w0, 1.f), T::template from_codes<false>(w1, 1.f),
+                                  T::template from_codes<true>(w1, 1.f)};
+                    k = __builtin_bit_cast(x8, w);
+                } else {
+                    k = __builtin_bit_cast(x8, kr[b][j]);
+                }
+#pragma unroll
+                for (int r = 0; r < RT; ++r) s[r][b] = T::mma16(k, q[r][j], s[r][b]);
+            }
+        }
+        const KeyPlace now = at;
+        if (tile + 4 < tiles) {
+            at = next;
+            fetch(at);
+            if (tile + 8 < tiles) next = find_key<E4M3>(a, it, head, it.begin + (tile + 8) * KT + lane % KT);
+        }
+        f32x4 over[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int at_key = 16 * b + 4 * g;
+            const f32x4 kc = E4M3 ? *reinterpret_cast<const f32x4 *>(key_c + at_key) : f32x4{a.c, a.c, a.c, a.c};
+            const f32x4 kl = E4M3 ? *reinterpret_cast<const f32x4 *>(key_log + at_key) : f32x4{0, 0, 0, 0};
+            if (E4M3) over[b] = *reinterpret_cast<const f32x4 *>(key_over + at_key);
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[r][b][i] = E4M3 ? __builtin_fmaf(s[r][b][i], kc[i], kl[i]) : s[r][b][i] * kc[i];
+                    if (!whole) {
+                        const uint32_t v = v0 + at_key + i, t = v < it.sinks ? v : v + it.gap;
+                        if (v >= it.end || !sees(a, position[r], t)) s[r][b][i] = -__builtin_inff();
+                    }
+                }
+        }
+        x8 p[RT][NB / 2];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            float top = s[r][0][0];
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[r][b][i]);
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            if (__any(top > m[r])) {
+                const float to = fmaxf(m[r], top), f = factor(m[r], to);
+                m[r] = to;
+                l[r] *= f;
+#pragma unroll
+                for (int d = 0; d < DC; ++d) o[r][d] *= f;
+            }
+            const float from = m[r] == -__builtin_inff() ? 0.f : m[r] - kLift<T>;
+#pragma unroll
+            for (int b = 0; b < NB; b += 2) {
+                u32x4 w;
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) {
+                    const int bb = b + i / 4;
+                    const float x = __builtin_amdgcn_exp2f(s[r][bb][i % 4] - from), y = __builtin_amdgcn_exp2f(s[r][bb][i % 4 + 1] - from);
+                    if (E4M3) l[r] = __builtin_fmaf(y, over[bb][i % 4 + 1], __builtin_fmaf(x, over[bb][i % 4], l[r]));
+                    else l[r] += x + y;
+                    w[i / 2] = narrow<T>(x, y);
+                }
+                p[r][b / 2] = __builtin_bit_cast(x8, w);
+            }
+        }
+        // outputs: lane (n, g) gets row n's elements 16 d + 4 g + i; the contraction's keys of lane group g are 4 g .. + 3 and 16 + 4 g .. + 3
+#pragma unroll
+        for (int u = 0; u < NB / 2; ++u)
+#pragma unroll
+            for (int d = 0; d < DC; ++d) {
+                u32x4 w;
+                if (E4M3) {
+                    const uint32_t j = n / 2, row = 32 * u + 4 * g + (j < 4 ? j : j + 12);
+                    const u32x2 c = read_columns8(mine + row * RB + ((d ^ (row & kSwizzle)) << 4) + (n & 1) * 8);
+                    w = u32x4{T::template from_codes<false>(c[0], 1.f), T::template from_codes<true>(c[0], 1.f), T::template from_codes<false>(c[1], 1.f),
+                              T::template from_codes<true>(c[1], 1.f)};
+                } else {
+                    const uint32_t row = 32 * u + 4 * g + n / 4;
+                    const u32x2 x = read_columns16(mine + row * RB + ((d ^ (row & kSwizzle)) << 5) + (n & 3) * 8);
+                    const u32x2 y = read_columns16(mine + (row + 16) * RB + ((d ^ ((row + 16) & kSwizzle)) << 5) + (n & 3) * 8);
+                    w = u32x4{x[0], x[1], y[0], y[1]};
+                }
+#pragma unroll
+                for (int r = 0; r < RT; ++r) o[r][d] = T::mma16(__builtin_bit_cast(x8, w), p[r][u], o[r][d]);
+            }
+        if (odd) {
+            for (uint32_t j = 0; j < KT && v0 + j < it.end; ++j) {
+                const uint32_t row = __shfl(now.row, (int)j), v = v0 + j, t = v < it.sinks ? v : v + it.gap;
+#pragma unroll
+                for (int d = 0; d < DC; ++d) {
+                    const f32x4 e = odd_values<T, E4M3, D>(a, head, row, 16 * d + 4 * g);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r)
+                        if (sees(a, position[r], t)) o[r][d] += e;
+                }
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+
+    // the wavefronts' results, joined
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        l[r] += __shfl_xor(l[r], 16);
+        l[r] += __shfl_xor(l[r], 32);
+        if (g == 0) state[wave][r * 16 + n] = f32x2{m[r], l[r]};
+    }
+    float *sums = reinterpret_cast<float *>(lds);
+    const uint32_t row = threadIdx.x / 16;
+    constexpr int E = D / 16;
+    const uint32_t dim = threadIdx.x % 16 * E;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        __syncthreads();                        // (nobody reads V, or the rows before, any more; the states are there)
+        float top = -__builtin_inff();
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, state[w][r * 16 + n][0]);
+        const float f = factor(m[r], top);
+#pragma unroll
+        for (int d = 0; d < DC; ++d) *reinterpret_cast<f32x4 *>(sums + (wave * 16 + n) * OS + 16 * d + 4 * g) = o[r][d] * f;
+        __syncthreads();
+        const uint32_t i = r * 16 + row;
+        if (i < it.n_rows) {
+            float most = -__builtin_inff(), sum = 0, e[E] = {};
+            for (int w = 0; w < 4; ++w) most = fmaxf(most, state[w][i][0]);
+            for (int w = 0; w < 4; ++w) {
+                sum += state[w][i][1] * factor(state[w][i][0], most);
+#pragma unroll
+                for (int j = 0; j < E; ++j) e[j] += sums[(w * 16 + row) * OS + dim + j];
+            }
+            if (it.pieces == 1) {
+                write_row<T, E>(a, it.token0, it.first_row + i, head, dim, D, sum, e);
+                if (dim == 0) write_lse<T>(a, it.token0, it.first_row + i, head, most, sum);
+            } else {
+                constexpr uint32_t kFloats = RT * 16 * (D + 2);
+                float *to = a.workspace + it.partial + (uint64_t)head * kFloats;
+#pragma unroll
+                for (int j = 0; j < E; ++j) to[i * D + dim + j] = e[j];
+                if (dim == 0) *reinterpret_cast<f32x2 *>(to + RT * 16 * D + 2 * i) = f32x2{most, sum};
+            }
+        }
+    }
+}
+
+// Many rows ------------------------------------------------------------------------------------------------------------------------
+//
+// 128 rows, 32 for each wavefront, against pieces of their keys in tiles of 64 that the wavefronts share in the LDS.  The matrix
+// instructions bound it, with the exponentials and the LDS's reads close behind.  A tile comes by way of registers, while the tile before is
+// worked on; 8-bit codes become T there, once for all rows, with their scales: exactly where these are powers of two, else with one more
+// rounding to T.
+template <typename T, bool E4M3>
+__device__ __forceinline__ void codes_to_half(u32x4 w, float scale, u32x4 *x, u32x4 *y) {
+    uint32_t e[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        e[2 * i] = T::template from_codes<false>(w[i], scale);
+        e[2 * i + 1] = T::template from_codes<true>(w[i], scale);
+    }
+    const uint32_t bits = __float_as_uint(scale);
+    if (__any((bits & 0x7fffffu) != 0)) {
+        const float rest = __uint_as_float((bits & 0x7fffffu) | 0x3f800000u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const f32x2 v = T::widen(e[i]);
+            e[i] = narrow<T>(v[0] * rest, v[1] * rest);
+        }
+    }
+    if (T::kExponent == F16::kExponent && __any(scale >= 128.f)) {         // beyond fp16's range: its largest
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if ((e[i] & 0x7fffu) == 0x7c00u) e[i] -= 1;
+            if ((e[i] & 0x7fff0000u) == 0x7c000000u) e[i] -= 0x10000u;
+        }
+    }
+    *x = u32x4{e[0], e[1], e[2], e[3]};
+    *y = u32x4{e[4], e[5], e[6], e[7]};
+}
+
+template <typename T, bool E4M3, int D>
+__global__ void __launch_bounds__(256, 2) kvl_attn_many_kernel(const AttnArgs a) {
+    constexpr int KT = kManyRowsTile;
+    constexpr int RB = 2 * D;                                       // bytes of a row in the LDS
+    constexpr int PR = D * (E4M3 ? 1 : 2) / 16;                     // pieces of a row in memory
+    constexpr int RP = 256 / PR;                                    // rows that the workgroup fetches at once
+    constexpr int N = KT / RP;                                      // a lane's pieces of a tile
+    constexpr int CH = D / 16, DB = D / 32;                         // steps of the first product; blocks of the output
+    constexpr int kSwizzle = D / 16 - 1;
+    static_assert(KT % RP == 0 && KT == 64, "whole pieces; a key a lane");
+    __shared__ __attribute__((aligned(16))) char lds[2][2][KT * RB];
+    __shared__ uint32_t odd_tile[3];
+    typedef typename T::x8 x8;
+
+    const AttnItem it = a.items[blockIdx.x / a.kv_heads];
+    const uint32_t head = blockIdx.x % a.kv_heads;
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 32, h = lane / 32;
+    const uint64_t row_pitch = (uint64_t)a.kv_heads * PR * 16;
+    const char *k_head = a.k + head * PR * 16, *v_head = a.v + head * PR * 16;
+    const uint32_t fetched = threadIdx.x / PR, piece = threadIdx.x % PR;
+
+    const uint32_t rows_before = wave * 32;
+    const bool works = rows_before < it.n_rows;
+    const uint32_t row = it.first_row + min(rows_before + n, it.n_rows - 1);
+    const uint32_t position = it.hit + row / a.group;
+    const uint32_t p0 = it.hit + it.first_row / a.group, p1 = it.hit + (it.first_row + it.n_rows - 1) / a.group;
+    const uint32_t w0 = it.hit + (it.first_row + min(rows_before, it.n_rows - 1)) / a.group,
+                   w1 = it.hit + (it.first_row + min(rows_before + 31, it.n_rows - 1)) / a.group;
+    x8 q[CH];
+    {
+        const char *from = a.q + 2 * ((it.token0 + row / a.group) * a.q_stride + (head * a.group + row % a.group) * D);
+#pragma unroll
+        for (int s = 0; s < CH; ++s) q[s] = *reinterpret_cast<const x8 *>(from + 2 * (16 * s + 8 * h));
+    }
+    f32x16 o[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0;
+    float m = -__builtin_inff(), l = 0;
+
+    u32x4 kr[N], vr[N];
+    auto fetch = [&](const KeyPlace &at) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint64_t from = __shfl(at.row, i * RP + fetched) * row_pitch + piece * 16;
+            kr[i] = *reinterpret_cast<const u32x4 *>(k_head + from);
+            vr[i] = *reinterpret_cast<const u32x4 *>(v_head + from);
+        }
+    };
+    if (threadIdx.x < 3) odd_tile[threadIdx.x] = 0;
+    __syncthreads();
+    const uint32_t tiles = (it.end - it.begin + KT - 1) / KT;
+    KeyPlace at{}, next{};
+    if (tiles) {
+        at = find_key<E4M3>(a, it, head, it.begin + lane);
+        fetch(at);
+        next = find_key<E4M3>(a, it, head, it.begin + KT + lane);
+    }
+    for (uint32_t tile = 0; tile < tiles; ++tile) {
+        const uint32_t v0 = it.begin + tile * KT;
+        char *k_lds = lds[tile % 2][0], *v_lds = lds[tile % 2][1];
+        // (infinities and NaN among values that not all rows see: as in the kernel above)
+        if (!all_seen(a, it, v0, v0 + KT - 1, p0, p1) && odd_pieces<T, E4M3>(vr)) {
+            odd_tile[tile % 3] = 1;
+            make_plain<T, E4M3>(vr);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t r = i * RP + fetched;
+            if (E4M3) {
+                u32x4 x, y;
+                codes_to_half<T, E4M3>(kr[i], __shfl(at.scale_k, (int)r), &x, &y);
+                *reinterpret_cast<u32x4 *>(k_lds + r * RB + (((2 * piece) ^ (r & 7)) << 4)) = x;
+                *reinterpret_cast<u32x4 *>(k_lds + r * RB + (((2 * piece + 1) ^ (r & 7)) << 4)) = y;
+                codes_to_half<T, E4M3>(vr[i], __shfl(at.scale_v, (int)r), &x, &y);
+                *reinterpret_cast<u32x4 *>(v_lds + r * RB + ((piece ^ (r & kSwizzle)) << 5)) = x;
+                *reinterpret_cast<u32x4 *>(v_lds + r * RB + ((piece ^ (r & kSwizzle)) << 5) + 16) = y;
+            } else {
+                *reinterpret_cast<u32x4 *>(k_lds + r * RB + ((piece ^ (r & 7)) << 4)) = kr[i];
+                *reinterpret_cast<u32x4 *>(v_lds + r * RB + (((piece >> 1) ^ (r & kSwizzle)) << 5) + ((piece & 1) << 4)) = vr[i];
+            }
+        }
+        const KeyPlace now = at;
+        if (tile + 1 < tiles) {
+            at = next;
+            fetch(at);
+            if (tile + 2 < tiles) next = find_key<E4M3>(a, it, head, v0 + 2 * KT + lane);
+        }
+        __syncthreads();
+        const bool odd = odd_tile[tile % 3] != 0;
+        if (threadIdx.x == 0) odd_tile[(tile + 2) % 3] = 0;
+
+        // a tile that none of the wavefront's rows sees
+        const uint32_t v1 = min(v0 + KT, it.end) - 1;
+        const uint32_t t0 = v0 < it.sinks ? v0 : v0 + it.gap, t1 = v1 < it.sinks ? v1 : v1 + it.gap;
+        if (!works || t0 > w1 || (t1 + a.window <= w0 && t0 >= a.sinks)) continue;
+        const bool whole = all_seen(a, it, v0, v0 + KT - 1, w0, w1);
+
+        // scores: lane (n, h) gets row n's of keys 32 b + 8 (i / 4) + 4 h + i % 4
+        f32x16 s[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[b][i] = 0;
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const x8 k = *reinterpret_cast<const x8 *>(k_lds + (32 * b + n) * RB + (((2 * j + h) ^ (n & 7)) << 4));
+                s[b] = T::mma32(k, q[j], s[b]);
+            }
+        }
+        if (!whole) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const uint32_t v = v0 + 32 * b + 8 * (i / 4) + 4 * h + i % 4, t = v < it.sinks ? v : v + it.gap;
+                    if (v >= it.end || !sees(a, position, t)) s[b][i] = -__builtin_inff();
+                }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+        top = fmaxf(top, __shfl_xor(top, 32)) * a.c;
+        if (__any(top > m)) {
+            const float to = fmaxf(m, top), f = factor(m, to);
+            m = to;
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= f;
+        }
+        const float from = m == -__builtin_inff() ? 0.f : kLift<T> - m;
+        x8 p[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            u32x4 w;
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u / 2][8 * (u % 2) + i], a.c, from));
+                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u / 2][8 * (u % 2) + i + 1], a.c, from));
+                l += x + y;
+                w[i / 2] = narrow<T>(x, y);
+            }
+            p[u] = __builtin_bit_cast(x8, w);
+        }
+        // outputs: lane (n, h) gets row n's elements 32 d + 8 (i / 4) + 4 h + i % 4
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                const uint32_t r = 16 * u + 4 * h + lane % 16 / 4, chunk = 2 * d + lane / 16 % 2;
+                const u32x2 x = read_columns16(v_lds + r * RB + ((chunk ^ (r & kSwizzle)) << 5) + (lane & 3) * 8);
+                const u32x2 y = read_columns16(v_lds + (r + 8) * RB + ((chunk ^ ((r + 8) & kSwizzle)) << 5) + (lane & 3) * 8);
+                o[d] = T::mma32(__builtin_bit_cast(x8, (u32x4{x[0], x[1], y[0], y[1]})), p[u], o[d]);
+            }
+        if (odd) {
+            for (uint32_t j = 0; j < KT && v0 + j < it.end; ++j) {
+                const uint32_t pool_row = __shfl(now.row, (int)j), v = v0 + j, t = v < it.sinks ? v : v + it.gap;
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const f32x4 e = odd_values<T, E4M3, D>(a, head, pool_row, 32 * d + 2 * i + 4 * h);
+                        if (sees(a, position, t))
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) o[d][i + x] += e[x];
+                    }
+            }
+        }
+    }
+
+    l += __shfl_xor(l, 32);
+    const uint32_t i = rows_before + n;
+    if (i >= it.n_rows) return;
+    if (it.pieces == 1) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int x = 0; x < 16; x += 4) {
+                const float e[4] = {o[d][x], o[d][x + 1], o[d][x + 2], o[d][x + 3]};
+                write_row<T, 4>(a, it.token0, row, head, 32 * d + 2 * x + 4 * h, D, l, e);
+            }
+        if (h == 0) write_lse<T>(a, it.token0, row, head, m, l);
+        return;
+    }
+    constexpr uint32_t kFloats = 128 * (D + 2);
+    float *to = a.workspace + it.partial + (uint64_t)head * kFloats;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int x = 0; x < 16; x += 4) *reinterpret_cast<f32x4 *>(to + i * D + 32 * d + 2 * x + 4 * h) = f32x4{o[d][x], o[d][x + 1], o[d][x + 2], o[d][x + 3]};
+    if (h == 0) *reinterpret_cast<f32x2 *>(to + 128 * D + 2 * i) = f32x2{m, l};
+}
+
+// Rows whose keys were cut: a wavefront a row, D / 64 elements a lane ----------------------------------------------------------------
+template <typename T, int D>
+__global__ void __launch_bounds__(256) kvl_attn_join_kernel(const AttnArgs a, const JoinItem *joins, uint32_t groups) {
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const JoinItem it = joins[blockIdx.x / groups / a.kv_heads];
+    const uint32_t head = blockIdx.x / groups % a.kv_heads, i = blockIdx.x % groups * 4 + wave;
+    if (i >= it.n_rows) return;
+    const uint32_t floats = it.tile_rows * (D + 2);
+    const uint64_t pitch = (uint64_t)a.kv_heads * floats;
+    const float *from = a.workspace + it.partial + (uint64_t)head * floats;
+    constexpr int E = D / 64;
+    float m = -__builtin_inff(), l = 0, e[2] = {0, 0};
+    for (uint32_t first = 0; first < it.pieces; first += 64) {
+        const uint32_t some = min(64u, it.pieces - first);
+        f32x2 state{-__builtin_inff(), 0};
+        if (lane < some) state = *reinterpret_cast<const f32x2 *>(from + (first + lane) * pitch + it.tile_rows * D + 2 * i);
+        float top = state[0];
+#pragma unroll
+        for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+        const float to = fmaxf(m, top), f = factor(m, to), mine = factor(state[0], to);
+        m = to;
+        float sum = state[1] * mine;
+#pragma unroll
+        for (int x = 32; x; x >>= 1) sum += __shfl_xor(sum, x);
+        l = l * f + sum;
+        e[0] *= f;
+        e[1] *= f;
+        const float *rows = from + first * pitch + i * D + lane * E;
+#pragma unroll 8
+        for (uint32_t k = 0; k < some; ++k) {
+            const float by = __shfl(mine, (int)k);
+            const float *at = rows + k * pitch;
+            e[0] = __builtin_fmaf(at[0], by, e[0]);
+            if (E == 2) e[1] = __builtin_fmaf(at[E - 1], by, e[1]);
+        }
+    }
+    const uint32_t row = it.first_row + i, token = it.token0 + row / a.group, h = head * a.group + row % a.group;
+    const float over = l == 0.f ? 0.f : 1.f / l;
+    const uint32_t w = narrow<T>(e[0] * over, e[1] * over);
+    char *to = a.out + 2 * (token * a.out_stride + (uint64_t)h * D + lane * E);
+    if (E == 2) *reinterpret_cast<uint32_t *>(to) = w;
+    else *reinterpret_cast<uint16_t *>(to) = (uint16_t)w;
+    if (lane == 0) write_lse<T>(a, it.token0, row, head, m, l);
+}
+
+}  // namespace kvl

@@ -284,6 +284,8 @@ struct DefaultStreamEvent;
 hipEvent_t launch_event(const kvl_plan_t *plan, hipStream_t stream, DefaultStreamEvent **passes);
 void launched(DefaultStreamEvent *passes, bool ok);
 void drop_stream_events(const kvl_plan_t *plan);
+// what a plan that goes away leaves to the library: its descriptor array, once its launches have run, and its events
+void release_plan(const kvl_plan_t *plan);
 // lanes come from, and go back to, a small pool shared by all plans
 hipStream_t take_pooled_lane(int device);
 void return_lane(hipStream_t lane, int device);

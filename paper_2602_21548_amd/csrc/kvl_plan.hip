@@ -374,6 +374,11 @@ static void descriptor_release(const kvl_plan_t *plan) {
     }
 }
 
+void release_plan(const kvl_plan_t *plan) {
+    if (plan->d_units) descriptor_release(plan);
+    drop_stream_events(plan);               // of a plan that never owned a descriptor array
+}
+
 int check_buffer(const kvl_plan_t *plan, const void *ptr, uint64_t bytes, bool allow_host) {
     if (plan->flags & KVL_NO_POINTER_CHECKS) return KVL_OK;
     return kvl_check_buffer(ptr, bytes, allow_host ? 1 : 0);
@@ -796,8 +801,7 @@ int kvl_plan_tuned(const kvl_layout_t *layout, const kvl_request_t *requests, ui
 
 void kvl_plan_destroy(kvl_plan_t *plan) {
     if (!plan) return;
-    if (plan->d_units) kvl::descriptor_release(plan);
-    kvl::drop_stream_events(plan);          // of a plan that never owned a descriptor array
+    kvl::release_plan(plan);
     for (hipStream_t s : plan->lanes) {
         // the lanes' work on this plan has normally ended (the stream the caller waits on follows
         // them); one that is still busy is waited for, it alone, since the plan's events go below
