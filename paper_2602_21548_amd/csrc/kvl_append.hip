@@ -1,9 +1,9 @@
 // New keys and values into a paged cache, rotated by their positions: kernels and entry point.
 //
-// Pairs (a, b) of a head's leading rope_dim elements become (a cos - b sin, b cos + a sin).  A lane takes 16 elements
-// that belong together: pieces of 8 at j and j + rope_dim/2 (halves), or 16 in a row (neighbours, and what is not rotated);
-// either way its 8 pairs' cosines and sines are 64 bytes in a row of the table, which the heads of a token share in the
-// caches.  Memory bounds both kernels: each element is read once and written once.
+// Pairs (a, b) of a head's leading rope_dim elements become (a cos - b sin, b cos + a sin).  A lane takes two pieces of 8 elements of a
+// head: those at j and j + rope_dim/2, whose elements are pairs (halves), else two that are half of what there is apart, so that neighbouring
+// lanes' pieces are neighbours in memory in each load and store.  The cosines and sines are a row of the table, which the heads of a token
+// share in the caches.  Memory bounds both kernels: each element is read once and written once.
 #include "kvl_attn_internal.h"
 #include "kvl_attn_types.h"
 
@@ -25,12 +25,18 @@ struct AppendArgs {
     uint32_t kv_heads, block_tokens, n_blocks;
 };
 
-// Where a lane's two pieces of 8 elements lie in a head.
+// A lane's two pieces of 8 elements of a head: where they begin, and which of them the rotation takes (from which pair of the table on).
+struct Pieces {
+    uint32_t first, second;
+    bool turn_first, turn_second;
+};
 template <int D>
-__device__ __forceinline__ void pieces_of(uint32_t p, uint32_t rope_dim, uint32_t pairs, bool turns, uint32_t *first, uint32_t *second, bool *rotate) {
-    *rotate = turns && p < rope_dim / 16;
-    *first = *rotate && pairs == KVL_ROPE_HALVES ? 8 * p : 16 * p;
-    *second = *rotate && pairs == KVL_ROPE_HALVES ? 8 * p + rope_dim / 2 : 16 * p + 8;
+__device__ __forceinline__ Pieces pieces_of(uint32_t p, uint32_t rope_dim, uint32_t pairs, bool turns) {
+    const uint32_t turned = turns ? rope_dim : 0;
+    if (pairs == KVL_ROPE_NEIGHBOURS) return {8 * p, 8 * p + D / 2, 8 * p < turned, 8 * p + D / 2 < turned};
+    if (16 * p < turned) return {8 * p, 8 * p + turned / 2, true, true};
+    const uint32_t x = 8 * (p - turned / 16) + turned;
+    return {x, x + (D - turned) / 2, false, false};
 }
 
 template <typename T, typename W>
@@ -45,26 +51,33 @@ __device__ __forceinline__ void widen16(u32x4 x, u32x4 y, W (&e)[16]) {
     }
 }
 
-// The 8 pairs of 16 elements turned by the angles of table row `position`, from pair 8 p on.
+// Pieces turned by the angles of table row `position`.
 template <typename W>
-__device__ __forceinline__ void turn(W (&e)[16], const float *rope, uint32_t position, uint32_t p, uint32_t rope_dim, uint32_t pairs) {
-    const f32x4 *cs = reinterpret_cast<const f32x4 *>(rope + (uint64_t)position * rope_dim + 16 * p);
-    f32x4 t[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) t[i] = cs[i];
+__device__ __forceinline__ void turn(W (&e)[16], const float *rope, uint32_t position, const Pieces &at, uint32_t rope_dim, uint32_t pairs) {
+    const float *row = rope + (uint64_t)position * rope_dim;
     if (pairs == KVL_ROPE_HALVES) {
+        if (!at.turn_first) return;
+        f32x4 t[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t[i] = reinterpret_cast<const f32x4 *>(row + 2 * at.first)[i];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const W c = t[j / 2][j % 2 * 2], s = t[j / 2][j % 2 * 2 + 1], a = e[j], b = e[8 + j];
             e[j] = a * c - b * s;
             e[8 + j] = b * c + a * s;
         }
-    } else {
+        return;
+    }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const W c = t[j / 2][j % 2 * 2], s = t[j / 2][j % 2 * 2 + 1], a = e[2 * j], b = e[2 * j + 1];
-            e[2 * j] = a * c - b * s;
-            e[2 * j + 1] = b * c + a * s;
+    for (int h = 0; h < 2; ++h) {
+        if (!(h ? at.turn_second : at.turn_first)) continue;
+        const f32x4 *from = reinterpret_cast<const f32x4 *>(row + (h ? at.second : at.first));
+        const f32x4 t[2] = {from[0], from[1]};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const W c = t[j / 2][j % 2 * 2], s = t[j / 2][j % 2 * 2 + 1], a = e[8 * h + 2 * j], b = e[8 * h + 2 * j + 1];
+            e[8 * h + 2 * j] = a * c - b * s;
+            e[8 * h + 2 * j + 1] = b * c + a * s;
         }
     }
 }
@@ -81,22 +94,20 @@ __device__ __forceinline__ void store16(char *to, uint32_t first, uint32_t secon
     *reinterpret_cast<u32x4 *>(to + 2 * second) = y;
 }
 
-// One task of 16 elements of a row of half-precision elements, turned where it has to be.
+// One lane's task: two pieces of a head, turned where they have to be.
 template <typename T, int D>
 __device__ __forceinline__ void half_task(const AppendArgs &a, const char *from, char *to, uint32_t p, uint32_t position, bool turns) {
-    uint32_t first, second;
-    bool rotate;
-    pieces_of<D>(p, a.rope_dim, a.rope_pairs, turns, &first, &second, &rotate);
-    const u32x4 x = *reinterpret_cast<const u32x4 *>(from + 2 * first), y = *reinterpret_cast<const u32x4 *>(from + 2 * second);
-    if (!rotate) {
-        *reinterpret_cast<u32x4 *>(to + 2 * first) = x;
-        *reinterpret_cast<u32x4 *>(to + 2 * second) = y;
+    const Pieces at = pieces_of<D>(p, a.rope_dim, a.rope_pairs, turns);
+    const u32x4 x = *reinterpret_cast<const u32x4 *>(from + 2 * at.first), y = *reinterpret_cast<const u32x4 *>(from + 2 * at.second);
+    if (!at.turn_first) {                       // (the second is not turned either)
+        *reinterpret_cast<u32x4 *>(to + 2 * at.first) = x;
+        *reinterpret_cast<u32x4 *>(to + 2 * at.second) = y;
         return;
     }
     float e[16];
     widen16<T>(x, y, e);
-    turn(e, a.rope, position, p, a.rope_dim, a.rope_pairs);
-    store16<T>(to, first, second, e);
+    turn(e, a.rope, position, at, a.rope_dim, a.rope_pairs);
+    store16<T>(to, at.first, at.second, e);
 }
 
 // Queries of any cache, keys and values of a 16-bit one: a lane a task, a token's queries, keys and values in a row.
@@ -126,112 +137,153 @@ __global__ void __launch_bounds__(256) kvl_append_half_kernel(const AppendArgs a
     append_half<T, D>(a, (uint64_t)blockIdx.x * blockDim.x + threadIdx.x);
 }
 
-// The code of e4m3 nearest to x / scale, where `over` is 1 / scale if that is exact and else 0.  x goes to 32 bits by
-// rounding to odd, so that the rounding to 8 that follows sees which side of a tie it was on.
-__device__ __forceinline__ float for_code(double x, double scale, double over) {
-    const double y = over != 0 ? x * over : x / scale;
-    float f = (float)fmin(fmax(y, -448.0), 448.0);
-    const double rest = y - (double)f;
+// A double as a float rounded to odd: a later rounding to fewer bits then sees which side of a tie, or of a border, it was on.
+__device__ __forceinline__ float to_odd(double x) {
+    const float f = (float)x;
+    const double rest = x - (double)f;
     const uint32_t bits = __float_as_uint(f);
-    if (rest != 0 && !(bits & 1u) && fabsf(f) >= 0x1p-20f && fabsf(f) < 448.f) f = __uint_as_float((rest > 0) == (f > 0) ? bits + 1 : bits - 1);
-    return f;
+    return rest != 0 && !(bits & 1u) && fabsf(f) >= 0x1p-120f && fabsf(f) < __builtin_inff() ? __uint_as_float((rest > 0) == (f > 0) ? bits + 1 : bits - 1) : f;
 }
-__device__ __forceinline__ uint32_t codes4(const double *x, double scale, double over) {
+
+// Four codes of e4m3: x / scale to the nearest, where x may have been rounded to odd.  `over` is 1 / scale if that is a power of two (the product
+// is exact then), else 0.
+__device__ __forceinline__ uint32_t codes4(const float *x, float scale, float over) {
     float f[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = for_code(x[i], scale, over);
+    for (int i = 0; i < 4; ++i) {
+        f[i] = over != 0 ? x[i] * over : to_odd((double)x[i] / (double)scale);
+        f[i] = fminf(fmaxf(f[i], -448.f), 448.f);
+    }
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
     w = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], w, true);
     uint32_t u = (uint32_t)w;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        if (!(fabs(x[i]) < __builtin_inf())) u |= 0x7fu << (8 * i);
+        if (!(fabsf(x[i]) < __builtin_inff())) u |= 0x7fu << (8 * i);
     return u;
 }
 
 // The least e in [-32, 63] with most <= 448 * 2^e: 448 is 1.75 * 2^8.
-__device__ __forceinline__ int least_exponent(double most) {
-    const uint64_t bits = __builtin_bit_cast(uint64_t, most);
-    if (bits == 0) return -32;
-    const int e = (int)(bits >> 52) - 1023 - ((bits & 0xfffffffffffffull) <= 0xc000000000000ull ? 8 : 7);
+__device__ __forceinline__ int least_exponent(float most) {
+    const uint32_t bits = __float_as_uint(most);
+    const int e = (int)(bits >> 23) - 127 - ((bits & 0x7fffffu) <= 0x600000u ? 8 : 7);
     return e < -32 ? -32 : e > 63 ? 63 : e;
 }
 
-// New rows of one block and head into an 8-bit plane.  The scale needs the largest of all of them first, so the rows are gone
-// through twice; the second time they come from the caches.  Rotated in 64 bits: the values' rounding to 8 bits is then that of
-// the exact ones (a 32-bit rotation moves about one code in a million), and 64-bit arithmetic is a small part of the time.
-template <typename T, int D>
-__device__ __forceinline__ void append_codes(const AppendArgs &a, const AppendBlock &b, uint32_t head, bool value, double *most_of_wave) {
-    constexpr uint32_t kHeadTasks = D / 16;
-    const uint64_t stride = value ? a.v_stride : a.k_stride;
-    const char *from = (value ? a.v : a.k) + 2 * (b.token * stride + head * D);
-    const uint64_t row0 = (uint64_t)b.block * a.block_tokens;
-    char *pool = (value ? a.pool_v : a.pool_k) + (row0 * a.kv_heads + head) * D;
-    const uint64_t row_bytes = (uint64_t)a.kv_heads * D;
-    float *scales = (value ? a.scale_v : a.scale_k) + (uint64_t)b.block * a.kv_heads + head;
-    const uint32_t position = a.tokens[b.token].position, n = b.n * kHeadTasks;
-    const float old = b.row ? *scales : 0.f;
+// What a workgroup does for one plane of a block and head.
+struct CodesPlane {
+    const char *from;           // new rows
+    char *pool;                 // the head's codes of the block's first row
+    float *scale;
+    uint64_t stride;            // bytes between new rows
+    bool value;
+};
 
-    auto load = [&](uint32_t i, double (&e)[16], uint32_t *first, uint32_t *second) {
-        const uint32_t row = i / kHeadTasks, p = i % kHeadTasks;
-        bool rotate;
-        pieces_of<D>(p, a.rope_dim, a.rope_pairs, !value, first, second, &rotate);
-        const char *x = from + 2 * row * stride;
-        widen16<T>(*reinterpret_cast<const u32x4 *>(x + 2 * *first), *reinterpret_cast<const u32x4 *>(x + 2 * *second), e);
-        if (rotate) turn(e, a.rope, position + row, p, a.rope_dim, a.rope_pairs);
+// New rows of one block and head into the 8-bit planes.  The scales need the largest of all their values first: rows of up to 64 (of heads of
+// 128) wait for it in registers, longer blocks' are read a second time, out of the caches.  Keys are rotated in 64 bits and rounded to odd in
+// 32: their codes are then those of the exact values (a rotation in 32 bits moves about one in a million), and all else goes by 32 bits.
+template <typename T, int D>
+__device__ __forceinline__ void append_codes(const AppendArgs &a, const AppendBlock &b, uint32_t head, f32x2 *most_of_wave) {
+    constexpr uint32_t kHeadTasks = D / 16;
+    constexpr int N = 2;                        // a lane's tasks of a plane that wait in registers
+    const uint64_t row0 = (uint64_t)b.block * a.block_tokens, row_bytes = (uint64_t)a.kv_heads * D, at_scale = (uint64_t)b.block * a.kv_heads + head;
+    const CodesPlane planes[2] = {
+        {a.k + 2 * (b.token * a.k_stride + head * D), a.pool_k + (row0 * a.kv_heads + head) * D, a.scale_k + at_scale, 2 * a.k_stride, false},
+        {a.v + 2 * (b.token * a.v_stride + head * D), a.pool_v + (row0 * a.kv_heads + head) * D, a.scale_v + at_scale, 2 * a.v_stride, true}};
+    const uint32_t position = b.position, n = b.n * kHeadTasks, per = blockDim.x;
+    float old[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) old[x] = b.row ? *planes[x].scale : 0.f;
+
+    auto load = [&](const CodesPlane &plane, uint32_t i, float (&e)[16]) {
+        const uint32_t row = i / kHeadTasks;
+        const Pieces at = pieces_of<D>(i % kHeadTasks, a.rope_dim, a.rope_pairs, !plane.value);
+        const char *x = plane.from + row * plane.stride;
+        const u32x4 first = *reinterpret_cast<const u32x4 *>(x + 2 * at.first), second = *reinterpret_cast<const u32x4 *>(x + 2 * at.second);
+        if (!at.turn_first) return widen16<T>(first, second, e);
+        double d[16];
+        widen16<T>(first, second, d);
+        turn(d, a.rope, position + row, at, a.rope_dim, a.rope_pairs);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) e[j] = to_odd(d[j]);
     };
-    double most = 0;
-    for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) {
-        double e[16];
-        uint32_t first, second;
-        load(i, e, &first, &second);
+    auto largest = [](const float (&e)[16], float most) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const double m = fabs(e[j]);
-            if (m < __builtin_inf()) most = fmax(most, m);
+        for (int j = 0; j < 16; ++j) most = fabsf(e[j]) < __builtin_inff() ? fmaxf(most, fabsf(e[j])) : most;
+        return most;
+    };
+    auto store = [&](const CodesPlane &plane, uint32_t i, const float (&e)[16], float scale, float over) {
+        const Pieces at = pieces_of<D>(i % kHeadTasks, a.rope_dim, a.rope_pairs, !plane.value);
+        char *to = plane.pool + (b.row + i / kHeadTasks) * row_bytes;
+        *reinterpret_cast<u32x2 *>(to + at.first) = u32x2{codes4(e, scale, over), codes4(e + 4, scale, over)};
+        *reinterpret_cast<u32x2 *>(to + at.second) = u32x2{codes4(e + 8, scale, over), codes4(e + 12, scale, over)};
+    };
+
+    float e[2][N][16], most[2] = {0, 0};
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const uint32_t i = threadIdx.x + j * per;
+            if (i >= n) continue;
+            load(planes[x], i, e[x][j]);
+            most[x] = largest(e[x][j], most[x]);
         }
-    }
+    for (uint32_t i = threadIdx.x + N * per; i < n; i += per)
+        for (int x = 0; x < 2; ++x) {
+            float w[16];
+            load(planes[x], i, w);
+            most[x] = largest(w, most[x]);
+        }
 #pragma unroll
-    for (int x = 32; x; x >>= 1) most = fmax(most, __shfl_xor(most, x));
-    if (blockDim.x > 64) {
-        __syncthreads();                        // (the plane before has read it)
-        if (threadIdx.x % 64 == 0) most_of_wave[threadIdx.x / 64] = most;
+    for (int x = 32; x; x >>= 1) {
+        most[0] = fmaxf(most[0], __shfl_xor(most[0], x));
+        most[1] = fmaxf(most[1], __shfl_xor(most[1], x));
+    }
+    if (per > 64) {
+        if (threadIdx.x % 64 == 0) most_of_wave[threadIdx.x / 64] = f32x2{most[0], most[1]};
         __syncthreads();
-        for (uint32_t w = 0; w < blockDim.x / 64; ++w) most = fmax(most, most_of_wave[w]);
-    }
-    const float fresh = __uint_as_float((uint32_t)(least_exponent(most) + 127) << 23);
-    const float scale = fmaxf(old, fresh);
-    const bool power = (__float_as_uint(scale) & 0x7fffffu) == 0;
-    const double over = power ? 1.0 / (double)scale : 0.0;
-    if (scale > old && b.row) {                 // the codes that are there, to the new scale
-        const double ratio = (double)old / (double)scale;
-        for (uint32_t i = threadIdx.x; i < b.row * kHeadTasks; i += blockDim.x) {
-            u32x4 *at = reinterpret_cast<u32x4 *>(pool + i / kHeadTasks * row_bytes + i % kHeadTasks * 16);
-            u32x4 w = *at;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const f32x2 x = widen_codes<0>(w[j]), y = widen_codes<1>(w[j]);
-                const double e[4] = {x[0] * ratio, x[1] * ratio, y[0] * ratio, y[1] * ratio};
-                w[j] = codes4(e, 1.0, 1.0);
-            }
-            *at = w;
+        for (uint32_t w = 0; w < per / 64; ++w) {
+            most[0] = fmaxf(most[0], most_of_wave[w][0]);
+            most[1] = fmaxf(most[1], most_of_wave[w][1]);
         }
     }
-    for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) {
-        double e[16];
-        uint32_t first, second;
-        load(i, e, &first, &second);
-        char *to = pool + (b.row + i / kHeadTasks) * row_bytes;
-        *reinterpret_cast<u32x2 *>(to + first) = u32x2{codes4(e, scale, over), codes4(e + 4, scale, over)};
-        *reinterpret_cast<u32x2 *>(to + second) = u32x2{codes4(e + 8, scale, over), codes4(e + 12, scale, over)};
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const CodesPlane &plane = planes[x];
+        const float scale = fmaxf(old[x], __uint_as_float((uint32_t)(least_exponent(most[x]) + 127) << 23));
+        const float over = (__float_as_uint(scale) & 0x7fffffu) == 0 ? 1.f / scale : 0.f;
+        if (scale > old[x] && b.row) {          // the codes that are there, to the new scale, which is a power of two
+            for (uint32_t i = threadIdx.x; i < b.row * kHeadTasks; i += per) {
+                u32x4 *at = reinterpret_cast<u32x4 *>(plane.pool + i / kHeadTasks * row_bytes + i % kHeadTasks * 16);
+                u32x4 w = *at;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const f32x2 c = widen_codes<0>(w[j]), d = widen_codes<1>(w[j]);
+                    const float was[4] = {to_odd((double)c[0] * old[x]), to_odd((double)c[1] * old[x]), to_odd((double)d[0] * old[x]), to_odd((double)d[1] * old[x])};
+                    w[j] = codes4(was, scale, over);
+                }
+                *at = w;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const uint32_t i = threadIdx.x + j * per;
+            if (i < n) store(plane, i, e[x][j], scale, over);
+        }
+        for (uint32_t i = threadIdx.x + N * per; i < n; i += per) {
+            float w[16];
+            load(plane, i, w);
+            store(plane, i, w, scale, over);
+        }
+        if (threadIdx.x == 0) *plane.scale = scale;
     }
-    if (threadIdx.x == 0) *scales = scale;
 }
 
 // 8-bit caches: a workgroup for each block that receives rows and each head, and after those workgroups for the queries.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) kvl_append_codes_kernel(const AppendArgs a) {
-    __shared__ double most_of_wave[4];
+    __shared__ f32x2 most_of_wave[4];
     const uint32_t work = a.n_blocks * a.kv_heads;
     if (blockIdx.x >= work) {
         append_half<T, D>(a, (uint64_t)(blockIdx.x - work) * blockDim.x + threadIdx.x);
@@ -239,9 +291,13 @@ __global__ void __launch_bounds__(256) kvl_append_codes_kernel(const AppendArgs 
     }
     const AppendBlock b = a.blocks[blockIdx.x / a.kv_heads];
     const uint32_t head = blockIdx.x % a.kv_heads;
-    append_codes<T, D>(a, b, head, false, most_of_wave);
-    append_codes<T, D>(a, b, head, true, most_of_wave);
+    append_codes<T, D>(a, b, head, most_of_wave);
 }
+
+// Up to so many tasks the queries go in the launch of an 8-bit cache's keys and values, beyond in one of their own: its kernel wants a third of
+// the registers.  (32 heads of 128 beside 8, us in one / two: 256 tasks a token, 512 tokens 13.8 / 17.5, 4096 29.3 / 37.0, 8192 59.7 / 65.0, 16384 114 /
+// 109, 32768 227 / 205.)
+constexpr uint64_t kOneLaunchTasks = 3u << 20;
 
 template <typename T, int D>
 static void launch_append(const kvl_attn_plan_t *plan, AppendArgs a, AttnLaunch &go) {
@@ -249,20 +305,21 @@ static void launch_append(const kvl_attn_plan_t *plan, AppendArgs a, AttnLaunch 
     a.q_tasks = a.q ? plan->layout.q_heads * (D / 16) : 0;
     a.kv_tasks = codes ? 0 : a.kv_heads * (D / 16);
     a.per_token = a.q_tasks + 2 * a.kv_tasks;
+    const uint64_t all = plan->new_tokens * a.per_token;
+    const uint32_t threads = plan->most_append_rows * (D / 16) <= 64 ? 64 : 256;
+    if (codes && all <= kOneLaunchTasks) {
+        a.tasks = all;
+        go(true, kvl_append_codes_kernel<T, D>, a.n_blocks * a.kv_heads + (uint32_t)((all + threads - 1) / threads), threads, a);
+        return;
+    }
+    if (codes) go(false, kvl_append_codes_kernel<T, D>, a.n_blocks * a.kv_heads, threads, a);
     // a launch has fewer than 2^32 lanes, and its tasks are numbered in 32 bits
-    const uint64_t most_tokens = a.per_token ? (1ull << 30) / a.per_token : plan->new_tokens;
+    const uint64_t most_tokens = (1ull << 30) / a.per_token;
     for (uint64_t t = 0; t < plan->new_tokens; t += most_tokens) {
         const uint64_t n = plan->new_tokens - t < most_tokens ? plan->new_tokens - t : most_tokens;
-        const bool last = t + n == plan->new_tokens;
         a.token_first = (uint32_t)t;
         a.tasks = n * a.per_token;
-        if (codes && t == 0) {
-            const uint32_t threads = plan->most_append_rows * (D / 16) <= 64 ? 64 : 256;
-            go(last, kvl_append_codes_kernel<T, D>, a.n_blocks * a.kv_heads + (uint32_t)((a.tasks + threads - 1) / threads), threads, a);
-        } else {
-            const uint32_t threads = 256;
-            go(last, kvl_append_half_kernel<T, D>, (uint32_t)((a.tasks + threads - 1) / threads), threads, a);
-        }
+        go(t + n == plan->new_tokens, kvl_append_half_kernel<T, D>, (uint32_t)((a.tasks + 255) / 256), 256, a);
     }
 }
 

@@ -19,13 +19,15 @@ static void launch_attn(const kvl_attn_plan_t *plan, AttnArgs a, AttnLaunch &go)
         const bool last = --left == 0;
         if (c == kRows16) go(last, kvl_attn_few_kernel<T, E4M3, D, 1>, groups, 256, a);
         else if (c == kRows32) go(last, kvl_attn_few_kernel<T, E4M3, D, 2>, groups, 256, a);
+        else if (c == kRows48) go(last, kvl_attn_few_kernel<T, E4M3, D, 3>, groups, 256, a);
         else if (c == kRows64) go(last, kvl_attn_few_kernel<T, E4M3, D, 4>, groups, 256, a);
         else go(last, kvl_attn_many_kernel<T, E4M3, D>, groups, 256, a);
     }
     if (plan->n_join) {
-        const uint32_t groups = (plan->most_join_rows + 3) / 4;
-        go(true, kvl_attn_join_kernel<T, D>, plan->n_join * a.kv_heads * groups, 256, a,
-           reinterpret_cast<const JoinItem *>(lists + plan->off_join), groups);
+        const JoinItem *joins = reinterpret_cast<const JoinItem *>(lists + plan->off_join);
+        const uint32_t groups = plan->join_groups(), all = plan->n_join * a.kv_heads * groups;
+        if (plan->join_waves() == 1) go(true, kvl_attn_join_kernel<T, D, 1>, all, 256, a, joins, groups);
+        else go(true, kvl_attn_join_kernel<T, D, 4>, all, 256, a, joins, groups);
     }
 }
 

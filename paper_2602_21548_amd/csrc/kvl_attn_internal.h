@@ -9,8 +9,8 @@
 namespace kvl {
 
 // Which kernel takes a request's rows (new tokens times the query heads that share a cache head), and in tiles of how many.
-enum AttnClass : uint32_t { kRows16 = 0, kRows32, kRows64, kRows128, kAttnClasses };
-constexpr uint32_t kClassRows[kAttnClasses] = {16, 32, 64, 128};
+enum AttnClass : uint32_t { kRows16 = 0, kRows32, kRows48, kRows64, kRows128, kAttnClasses };
+constexpr uint32_t kClassRows[kAttnClasses] = {16, 32, 48, 64, 128};
 
 // One piece of work of the attention kernels, for every cache head (kvl_attn_item_t, with what a kernel would have to look up).
 struct AttnItem {
@@ -44,8 +44,10 @@ struct AppendBlock {
     uint32_t token;
     uint32_t row;
     uint32_t n;
+    uint32_t position;      // of `token`
+    uint32_t reserved[3];
 };
-static_assert(sizeof(AppendBlock) == 16, "one descriptor unit");
+static_assert(sizeof(AppendBlock) == 32, "two descriptor units");
 
 struct AppendToken {
     uint32_t position;
@@ -55,8 +57,8 @@ struct AppendToken {
 // Floats of a partial result of a tile: unnormalised outputs, then each row's maximum and sum.
 inline uint64_t partial_floats(uint32_t tile_rows, uint32_t head_dim) { return (uint64_t)tile_rows * (head_dim + 2); }
 
-// Keys of a tile of one wavefront in the kernel for few rows: 8 KB of K, 4 KB with 8-bit heads of 64.
-constexpr uint32_t few_rows_tile(bool e4m3, uint32_t head_dim) { return e4m3 || head_dim == 64 ? 64 : 32; }
+// Keys of a tile of one wavefront in the kernel for few rows: 8 KB of K, 4 KB of 8-bit ones.
+constexpr uint32_t few_rows_tile(uint32_t head_dim) { return head_dim == 64 ? 64 : 32; }
 constexpr uint32_t kManyRowsTile = 64;
 
 }  // namespace kvl
@@ -70,10 +72,14 @@ struct kvl_attn_plan_s {
     uint64_t workspace_bytes = 0;
     std::vector<kvl_attn_item_t> items;                 // as the public call gives them
     uint32_t class_first[kvl::kAttnClasses + 1] = {};   // items of each class
-    uint32_t n_join = 0, most_join_rows = 0, n_append_blocks = 0, most_append_rows = 0;
+    uint32_t n_join = 0, most_join_rows = 0, most_pieces = 0, n_append_blocks = 0, most_append_rows = 0;
     uint64_t off_items = 0, off_join = 0, off_tables = 0, off_blocks = 0, off_tokens = 0;    // bytes into the device array
     uint64_t div_mul = 0;                               // t / block_tokens == t * div_mul >> div_shift for t < 2^31
     uint32_t div_shift = 0;
+
+    // the join's wavefronts for each row, and its workgroups for each tile of rows and head
+    uint32_t join_waves() const { return most_pieces > 8 ? 4 : 1; }
+    uint32_t join_groups() const { return join_waves() == 4 ? most_join_rows : (most_join_rows + 3) / 4; }
 };
 
 namespace kvl {

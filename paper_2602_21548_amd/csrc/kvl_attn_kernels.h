@@ -36,13 +36,24 @@ struct AttnArgs {
 };
 
 constexpr float kLowestScale = 0x1p-32f, kHighestScale = 0x1p63f;
-// Weights of fp16 are 2^8 times those of the formula: what is small beside the largest stays above fp16's least normal for longer.
+// A row's maximum is raised, and what it has so far multiplied, only where a score is beyond it by more than this (in powers of two): weights
+// are then at most 2^8, which costs no bits, and most tiles raise nothing.
+constexpr float kSlack = 8.f;
+// Weights of fp16 are 2^6 times those of the formula: what is small beside the largest stays above fp16's least normal for longer.
 template <typename T>
 constexpr float kLift = 0.f;
 template <>
-constexpr float kLift<F16> = 8.f;
+constexpr float kLift<F16> = 6.f;
 
-typedef __attribute__((address_space(3))) char *lds_ptr;
+// The largest of the values of two lanes 32 apart, and of four lanes 16 apart.
+__device__ __forceinline__ float max_halves(float x) {
+    const u32x2 both = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+}
+__device__ __forceinline__ float max_quarters(float x) {
+    const u32x2 both = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return max_halves(fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])));
+}
 
 // 4 elements of a column out of the 16-lane group's 4 rows of 16: lane i of the group names 8 bytes, row i / 4, and gets column i.
 __device__ __forceinline__ u32x2 read_columns16(const char *at) {
@@ -56,25 +67,39 @@ __device__ __forceinline__ u32x2 read_columns8(const char *at) {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((ptr)(const_cast<char *>(at))));
 }
 
-// Where a key lies, and what its codes are multiplied by.
+// The item and head of a workgroup.  Workgroups go to the 8 XCDs in turn.  `TOGETHER`: the heads of one item, which lie side by side in
+// the rows of the pool, are taken by one XCD, one after the other.  That suits short pieces of rows (8-bit heads of 128, 64 requests of 16-64 K
+// tokens, 957 us against 1075) and not long ones (16-bit heads of 128 under a window of 4096, 376 us against 363).
+template <bool TOGETHER>
+__device__ __forceinline__ void place_of(uint32_t group, uint32_t groups, uint32_t heads, uint32_t *item, uint32_t *head) {
+    if (TOGETHER && group < groups / (8 * heads) * (8 * heads)) {
+        *item = group / 8 / heads * 8 + group % 8;
+        *head = group / 8 % heads;
+    } else {
+        *item = group / heads;
+        *head = group % heads;
+    }
+}
+
+// Where a key lies.  Its block's number is a load, and what is loaded by that number comes an iteration later: loads are waited for in
+// their order, so one that needs another's result at once would wait for all keys and values on their way, too.
 struct KeyPlace {
-    uint32_t row;
-    float scale_k, scale_v;
+    uint32_t block, row_in_block;
 };
-template <bool E4M3>
-__device__ __forceinline__ KeyPlace find_key(const AttnArgs &a, const AttnItem &it, uint32_t head, uint32_t place) {
+__device__ __forceinline__ KeyPlace find_key(const AttnArgs &a, const AttnItem &it, uint32_t place) {
     const uint32_t v = min(place, it.end - 1), t = v < it.sinks ? v : v + it.gap;
     const uint32_t b = (uint32_t)((t * a.div_mul) >> a.div_shift);
-    const uint32_t id = (uint32_t)a.tables[it.table + b];
-    KeyPlace k;
-    k.row = id * a.block_tokens + (t - b * a.block_tokens);
-    if (E4M3) {
-        const uint64_t at = (uint64_t)id * a.kv_heads + head;
-        k.scale_k = fminf(fmaxf(a.scale_k[at], kLowestScale), kHighestScale);
-        k.scale_v = fminf(fmaxf(a.scale_v[at], kLowestScale), kHighestScale);
-    }
-    return k;
+    return {(uint32_t)a.tables[it.table + b], t - b * a.block_tokens};
 }
+// What a block's codes are multiplied by.
+struct Scales {
+    float k, v;
+};
+__device__ __forceinline__ Scales load_scales(const AttnArgs &a, uint32_t block, uint32_t head) {
+    const uint64_t at = (uint64_t)block * a.kv_heads + head;
+    return {a.scale_k[at], a.scale_v[at]};
+}
+__device__ __forceinline__ float in_range(float scale) { return fminf(fmaxf(scale, kLowestScale), kHighestScale); }
 
 __device__ __forceinline__ bool sees(const AttnArgs &a, uint32_t position, uint32_t t) {
     return t <= position && (t + a.window > position || t < a.sinks);
@@ -172,8 +197,8 @@ __device__ __forceinline__ void write_lse(const AttnArgs &a, uint32_t token0, ui
 // scales multiply scores (K) and join the exponent (V: with x = c s_k <q, K_t> + log2 s_v, 2^(x - m) multiplies the codes, and 2^(x - m) / s_v
 // is the term of l), in 32 bits, whatever T is.
 template <typename T, bool E4M3, int D, int RT>
-__global__ void __launch_bounds__(256) kvl_attn_few_kernel(const AttnArgs a) {
-    constexpr int KT = few_rows_tile(E4M3, D), NB = KT / 16;        // keys of a tile, blocks of 16
+__global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) {
+    constexpr int KT = few_rows_tile(D), NB = KT / 16;        // keys of a tile, blocks of 16
     constexpr int RB = D * (E4M3 ? 1 : 2);                          // bytes of a row
     constexpr int PR = RB / 16;                                     // pieces of 16 bytes in it
     constexpr int VP = KT * PR / 64;                                // a lane's pieces of V
@@ -186,29 +211,17 @@ __global__ void __launch_bounds__(256) kvl_attn_few_kernel(const AttnArgs a) {
     __shared__ __attribute__((aligned(16))) char lds[kBytes];
     __shared__ f32x2 state[4][RT * 16];
     typedef typename T::x8 x8;
+    __shared__ x8 staged[RT > 1 ? RT * CH : 1][64];
 
-    const AttnItem it = a.items[blockIdx.x / a.kv_heads];
-    const uint32_t head = blockIdx.x % a.kv_heads;
+    uint32_t item, head;
+    place_of<(RB < 256)>(blockIdx.x, gridDim.x, a.kv_heads, &item, &head);
+    const AttnItem it = a.items[item];
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 16, g = lane / 16;
     char *mine = lds + wave * kWaveBytes;
     float *key_c = reinterpret_cast<float *>(mine + KT * RB), *key_log = key_c + KT, *key_over = key_log + KT;
     const uint64_t row_pitch = (uint64_t)a.kv_heads * RB;
     const char *k_head = a.k + head * RB, *v_head = a.v + head * RB;
 
-    x8 q[RT][CH];
-    uint32_t position[RT];
-    const uint32_t p0 = it.hit + it.first_row / a.group, p1 = it.hit + (it.first_row + it.n_rows - 1) / a.group;
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        const uint32_t i = min(r * 16 + n, it.n_rows - 1), row = it.first_row + i, token = row / a.group;
-        position[r] = it.hit + token;
-        const char *from = a.q + 2 * ((it.token0 + token) * a.q_stride + (head * a.group + row % a.group) * D);
-#pragma unroll
-        for (int s = 0; s < CH; ++s) {
-            const uint32_t dim = E4M3 ? (g + 4 * (s / 2)) * 16 + s % 2 * 8 : s * 32 + g * 8;
-            q[r][s] = *reinterpret_cast<const x8 *>(from + 2 * dim);
-        }
-    }
     f32x4 o[RT][DC];
     float m[RT], l[RT];
 #pragma unroll
@@ -219,25 +232,47 @@ __global__ void __launch_bounds__(256) kvl_attn_few_kernel(const AttnArgs a) {
         for (int d = 0; d < DC; ++d) o[r][d] = f32x4{0, 0, 0, 0};
     }
 
-    u32x4 kr[NB][KP], vr[VP];
+    u32x4 kr[NB][KP], kn[NB][KP], vr[VP];
+    Scales scales{};
+    uint32_t rows = 0;                          // of the tile on its way, a lane each
     auto fetch = [&](const KeyPlace &at) {
+        rows = at.block * a.block_tokens + at.row_in_block;
+        if (E4M3) scales = load_scales(a, at.block, head);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            const char *from = k_head + __shfl(at.row, 16 * b + n) * row_pitch + g * 16;
+            const char *from = k_head + __shfl(rows, 16 * b + n) * row_pitch + g * 16;
 #pragma unroll
-            for (int i = 0; i < KP; ++i) kr[b][i] = *reinterpret_cast<const u32x4 *>(from + 64 * i);
+            for (int i = 0; i < KP; ++i) kn[b][i] = *reinterpret_cast<const u32x4 *>(from + 64 * i);
         }
 #pragma unroll
-        for (int i = 0; i < VP; ++i) vr[i] = *reinterpret_cast<const u32x4 *>(v_head + __shfl(at.row, (i * 64 + lane) / PR) * row_pitch + lane % PR * 16);
+        for (int i = 0; i < VP; ++i) vr[i] = *reinterpret_cast<const u32x4 *>(v_head + __shfl(rows, (i * 64 + lane) / PR) * row_pitch + lane % PR * 16);
     };
 
     const uint32_t tiles = (it.end - it.begin + KT - 1) / KT;
-    KeyPlace at{}, next{};
+    KeyPlace next{};
     if (wave < tiles) {
-        at = find_key<E4M3>(a, it, head, it.begin + wave * KT + lane % KT);
-        fetch(at);
-        next = find_key<E4M3>(a, it, head, it.begin + (wave + 4) * KT + lane % KT);
+        const KeyPlace first = find_key(a, it, it.begin + wave * KT + lane % KT);
+        next = find_key(a, it, it.begin + (wave + 4) * KT + lane % KT);
+        fetch(first);
     }
+    // Queries: in registers for 16 rows, else in the LDS, in the order in which the matrix instructions take them.
+    constexpr bool kStaged = RT > 1;
+    x8 q[kStaged ? 1 : CH];
+    uint32_t position[RT];
+    const uint32_t p0 = it.hit + it.first_row / a.group, p1 = it.hit + (it.first_row + it.n_rows - 1) / a.group;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const uint32_t i = min(r * 16 + n, it.n_rows - 1), row = it.first_row + i, token = row / a.group;
+        position[r] = it.hit + token;
+        const char *from = a.q + 2 * ((it.token0 + token) * a.q_stride + (head * a.group + row % a.group) * D);
+#pragma unroll
+        for (int s = 0; s < CH; ++s) {
+            const uint32_t dim = E4M3 ? (g + 4 * (s / 2)) * 16 + s % 2 * 8 : s * 32 + g * 8;
+            if (!kStaged) q[s] = *reinterpret_cast<const x8 *>(from + 2 * dim);
+            else if (wave == (uint32_t)(r * CH + s) % 4) staged[r * CH + s][lane] = *reinterpret_cast<const x8 *>(from + 2 * dim);
+        }
+    }
+    if (kStaged) __syncthreads();
     for (uint32_t tile = wave; tile < tiles; tile += 4) {
         const uint32_t v0 = it.begin + tile * KT;
         const bool whole = all_seen(a, it, v0, v0 + KT - 1, p0, p1);
@@ -253,68 +288,64 @@ __global__ void __launch_bounds__(256) kvl_attn_few_kernel(const AttnArgs a) {
         }
         if (E4M3) {
             if (lane < KT) {
-                key_c[lane] = a.c * at.scale_k;
-                key_log[lane] = __log2f(at.scale_v);
-                key_over[lane] = 1.f / at.scale_v;
+                const float by = in_range(scales.v);
+                key_c[lane] = a.c * in_range(scales.k);
+                key_log[lane] = __log2f(by);
+                key_over[lane] = 1.f / by;
             }
         }
         __builtin_amdgcn_wave_barrier();
-        // scores: lane (n, g) gets row n's of keys 16 b + 4 g + i
-        f32x4 s[RT][NB];
+        const uint32_t now_rows = rows;
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int r = 0; r < RT; ++r) s[r][b] = f32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int j = 0; j < CH; ++j) {
-                x8 k;
-                if (E4M3) {
-                    const uint32_t w0 = kr[b][j / 2][j % 2 * 2], w1 = kr[b][j / 2][j % 2 * 2 + 1];
-                    const u32x4 w{T::template from_codes<false>(w0, 1.f), T::template from_codes<true>(w0, 1.f), T::template from_codes<false>(w1, 1.f),
-                                  T::template from_codes<true>(w1, 1.f)};
-                    k = __builtin_bit_cast(x8, w);
-                } else {
-                    k = __builtin_bit_cast(x8, kr[b][j]);
-                }
-#pragma unroll
-                for (int r = 0; r < RT; ++r) s[r][b] = T::mma16(k, q[r][j], s[r][b]);
-            }
-        }
-        const KeyPlace now = at;
+            for (int i = 0; i < KP; ++i) kr[b][i] = kn[b][i];
+        // the next tile comes while this one is worked on
         if (tile + 4 < tiles) {
-            at = next;
-            fetch(at);
-            if (tile + 8 < tiles) next = find_key<E4M3>(a, it, head, it.begin + (tile + 8) * KT + lane % KT);
+            fetch(next);
+            if (tile + 8 < tiles) next = find_key(a, it, it.begin + (tile + 8) * KT + lane % KT);
         }
-        f32x4 over[NB];
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int at_key = 16 * b + 4 * g;
-            const f32x4 kc = E4M3 ? *reinterpret_cast<const f32x4 *>(key_c + at_key) : f32x4{a.c, a.c, a.c, a.c};
-            const f32x4 kl = E4M3 ? *reinterpret_cast<const f32x4 *>(key_log + at_key) : f32x4{0, 0, 0, 0};
-            if (E4M3) over[b] = *reinterpret_cast<const f32x4 *>(key_over + at_key);
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    s[r][b][i] = E4M3 ? __builtin_fmaf(s[r][b][i], kc[i], kl[i]) : s[r][b][i] * kc[i];
-                    if (!whole) {
-                        const uint32_t v = v0 + at_key + i, t = v < it.sinks ? v : v + it.gap;
-                        if (v >= it.end || !sees(a, position[r], t)) s[r][b][i] = -__builtin_inff();
-                    }
-                }
-        }
-        x8 p[RT][NB / 2];
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            float top = s[r][0][0];
+            // scores: lane (n, g) gets row n's of keys 16 b + 4 g + i
+            f32x4 s[NB];
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
+            for (int b = 0; b < NB; ++b) s[b] = f32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[r][b][i]);
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            if (__any(top > m[r])) {
+            for (int j = 0; j < CH; ++j) {
+                const x8 x = kStaged ? staged[r * CH + j][lane] : q[kStaged ? 0 : j];
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    x8 k;
+                    if (E4M3) {
+                        const uint32_t w0 = kr[b][j / 2][j % 2 * 2], w1 = kr[b][j / 2][j % 2 * 2 + 1];
+                        const u32x4 w{T::template from_codes<false>(w0, 1.f), T::template from_codes<true>(w0, 1.f), T::template from_codes<false>(w1, 1.f),
+                                      T::template from_codes<true>(w1, 1.f)};
+                        k = __builtin_bit_cast(x8, w);
+                    } else {
+                        k = __builtin_bit_cast(x8, kr[b][j]);
+                    }
+                    s[b] = T::mma16(k, x, s[b]);
+                }
+            }
+            float top = -__builtin_inff();
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const int at_key = 16 * b + 4 * g;
+                const f32x4 kc = E4M3 ? *reinterpret_cast<const f32x4 *>(key_c + at_key) : f32x4{a.c, a.c, a.c, a.c};
+                const f32x4 kl = E4M3 ? *reinterpret_cast<const f32x4 *>(key_log + at_key) : f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[b][i] = E4M3 ? __builtin_fmaf(s[b][i], kc[i], kl[i]) : s[b][i] * kc[i];
+                    if (!whole) {
+                        const uint32_t v = v0 + at_key + i, t = v < it.sinks ? v : v + it.gap;
+                        if (v >= it.end || !sees(a, position[r], t)) s[b][i] = -__builtin_inff();
+                    }
+                    top = fmaxf(top, s[b][i]);
+                }
+            }
+            top = max_quarters(top);
+            if (__any(top > m[r] + kSlack)) {
                 const float to = fmaxf(m[r], top), f = factor(m[r], to);
                 m[r] = to;
                 l[r] *= f;
@@ -322,43 +353,47 @@ __global__ void __launch_bounds__(256) kvl_attn_few_kernel(const AttnArgs a) {
                 for (int d = 0; d < DC; ++d) o[r][d] *= f;
             }
             const float from = m[r] == -__builtin_inff() ? 0.f : m[r] - kLift<T>;
+            x8 p[NB / 2];
 #pragma unroll
             for (int b = 0; b < NB; b += 2) {
                 u32x4 w;
 #pragma unroll
-                for (int i = 0; i < 8; i += 2) {
-                    const int bb = b + i / 4;
-                    const float x = __builtin_amdgcn_exp2f(s[r][bb][i % 4] - from), y = __builtin_amdgcn_exp2f(s[r][bb][i % 4 + 1] - from);
-                    if (E4M3) l[r] = __builtin_fmaf(y, over[bb][i % 4 + 1], __builtin_fmaf(x, over[bb][i % 4], l[r]));
-                    else l[r] += x + y;
-                    w[i / 2] = narrow<T>(x, y);
+                for (int bb = b; bb < b + 2; ++bb) {
+                    const f32x4 over = E4M3 ? *reinterpret_cast<const f32x4 *>(key_over + 16 * bb + 4 * g) : f32x4{1, 1, 1, 1};
+#pragma unroll
+                    for (int i = 0; i < 4; i += 2) {
+                        const float x = __builtin_amdgcn_exp2f(s[bb][i] - from), y = __builtin_amdgcn_exp2f(s[bb][i + 1] - from);
+                        if (E4M3) l[r] = __builtin_fmaf(y, over[i + 1], __builtin_fmaf(x, over[i], l[r]));
+                        else l[r] += x + y;
+                        w[bb % 2 * 2 + i / 2] = narrow<T>(x, y);
+                    }
                 }
-                p[r][b / 2] = __builtin_bit_cast(x8, w);
+                p[b / 2] = __builtin_bit_cast(x8, w);
             }
+            // outputs: lane (n, g) gets row n's elements 16 d + 4 g + i; the contraction's keys of lane group g are 4 g .. + 3 and 16 + 4 g .. + 3
+#pragma unroll
+            for (int u = 0; u < NB / 2; ++u)
+#pragma unroll
+                for (int d = 0; d < DC; ++d) {
+                    u32x4 w;
+                    if (E4M3) {
+                        const uint32_t j = n / 2, row = 32 * u + 4 * g + (j < 4 ? j : j + 12);
+                        const u32x2 c = read_columns8(mine + row * RB + ((d ^ (row & kSwizzle)) << 4) + (n & 1) * 8);
+                        w = u32x4{T::template from_codes<false>(c[0], 1.f), T::template from_codes<true>(c[0], 1.f), T::template from_codes<false>(c[1], 1.f),
+                                  T::template from_codes<true>(c[1], 1.f)};
+                    } else {
+                        const uint32_t row = 32 * u + 4 * g + n / 4;
+                        const u32x2 x = read_columns16(mine + row * RB + ((d ^ (row & kSwizzle)) << 5) + (n & 3) * 8);
+                        const u32x2 y = read_columns16(mine + (row + 16) * RB + ((d ^ ((row + 16) & kSwizzle)) << 5) + (n & 3) * 8);
+                        w = u32x4{x[0], x[1], y[0], y[1]};
+                    }
+                    o[r][d] = T::mma16(__builtin_bit_cast(x8, w), p[u], o[r][d]);
+                }
+            if (RT > 2) __builtin_amdgcn_sched_barrier(0);      // (one row tile's scores at a time in the registers)
         }
-        // outputs: lane (n, g) gets row n's elements 16 d + 4 g + i; the contraction's keys of lane group g are 4 g .. + 3 and 16 + 4 g .. + 3
-#pragma unroll
-        for (int u = 0; u < NB / 2; ++u)
-#pragma unroll
-            for (int d = 0; d < DC; ++d) {
-                u32x4 w;
-                if (E4M3) {
-                    const uint32_t j = n / 2, row = 32 * u + 4 * g + (j < 4 ? j : j + 12);
-                    const u32x2 c = read_columns8(mine + row * RB + ((d ^ (row & kSwizzle)) << 4) + (n & 1) * 8);
-                    w = u32x4{T::template from_codes<false>(c[0], 1.f), T::template from_codes<true>(c[0], 1.f), T::template from_codes<false>(c[1], 1.f),
-                              T::template from_codes<true>(c[1], 1.f)};
-                } else {
-                    const uint32_t row = 32 * u + 4 * g + n / 4;
-                    const u32x2 x = read_columns16(mine + row * RB + ((d ^ (row & kSwizzle)) << 5) + (n & 3) * 8);
-                    const u32x2 y = read_columns16(mine + (row + 16) * RB + ((d ^ ((row + 16) & kSwizzle)) << 5) + (n & 3) * 8);
-                    w = u32x4{x[0], x[1], y[0], y[1]};
-                }
-#pragma unroll
-                for (int r = 0; r < RT; ++r) o[r][d] = T::mma16(__builtin_bit_cast(x8, w), p[r][u], o[r][d]);
-            }
         if (odd) {
             for (uint32_t j = 0; j < KT && v0 + j < it.end; ++j) {
-                const uint32_t row = __shfl(now.row, (int)j), v = v0 + j, t = v < it.sinks ? v : v + it.gap;
+                const uint32_t row = __shfl(now_rows, (int)j), v = v0 + j, t = v < it.sinks ? v : v + it.gap;
 #pragma unroll
                 for (int d = 0; d < DC; ++d) {
                     const f32x4 e = odd_values<T, E4M3, D>(a, head, row, 16 * d + 4 * g);
@@ -392,24 +427,23 @@ __global__ void __launch_bounds__(256) kvl_attn_few_kernel(const AttnArgs a) {
         for (int d = 0; d < DC; ++d) *reinterpret_cast<f32x4 *>(sums + (wave * 16 + n) * OS + 16 * d + 4 * g) = o[r][d] * f;
         __syncthreads();
         const uint32_t i = r * 16 + row;
-        if (i < it.n_rows) {
-            float most = -__builtin_inff(), sum = 0, e[E] = {};
-            for (int w = 0; w < 4; ++w) most = fmaxf(most, state[w][i][0]);
-            for (int w = 0; w < 4; ++w) {
-                sum += state[w][i][1] * factor(state[w][i][0], most);
+        if (i >= it.n_rows) continue;
+        float most = -__builtin_inff(), sum = 0, e[E] = {};
+        for (int w = 0; w < 4; ++w) most = fmaxf(most, state[w][i][0]);
+        for (int w = 0; w < 4; ++w) {
+            sum += state[w][i][1] * factor(state[w][i][0], most);
 #pragma unroll
-                for (int j = 0; j < E; ++j) e[j] += sums[(w * 16 + row) * OS + dim + j];
-            }
-            if (it.pieces == 1) {
-                write_row<T, E>(a, it.token0, it.first_row + i, head, dim, D, sum, e);
-                if (dim == 0) write_lse<T>(a, it.token0, it.first_row + i, head, most, sum);
-            } else {
-                constexpr uint32_t kFloats = RT * 16 * (D + 2);
-                float *to = a.workspace + it.partial + (uint64_t)head * kFloats;
+            for (int j = 0; j < E; ++j) e[j] += sums[(w * 16 + row) * OS + dim + j];
+        }
+        if (it.pieces == 1) {
+            write_row<T, E>(a, it.token0, it.first_row + i, head, dim, D, sum, e);
+            if (dim == 0) write_lse<T>(a, it.token0, it.first_row + i, head, most, sum);
+        } else {
+            constexpr uint32_t kFloats = RT * 16 * (D + 2);
+            float *to = a.workspace + it.partial + (uint64_t)head * kFloats;
 #pragma unroll
-                for (int j = 0; j < E; ++j) to[i * D + dim + j] = e[j];
-                if (dim == 0) *reinterpret_cast<f32x2 *>(to + RT * 16 * D + 2 * i) = f32x2{most, sum};
-            }
+            for (int j = 0; j < E; ++j) to[i * D + dim + j] = e[j];
+            if (dim == 0) *reinterpret_cast<f32x2 *>(to + RT * 16 * D + 2 * i) = f32x2{most, sum};
         }
     }
 }
@@ -449,7 +483,7 @@ __device__ __forceinline__ void codes_to_half(u32x4 w, float scale, u32x4 *x, u3
 }
 
 template <typename T, bool E4M3, int D>
-__global__ void __launch_bounds__(256, 2) kvl_attn_many_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(const AttnArgs a) {
     constexpr int KT = kManyRowsTile;
     constexpr int RB = 2 * D;                                       // bytes of a row in the LDS
     constexpr int PR = D * (E4M3 ? 1 : 2) / 16;                     // pieces of a row in memory
@@ -490,10 +524,14 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_many_kernel(const AttnArgs a)
     float m = -__builtin_inff(), l = 0;
 
     u32x4 kr[N], vr[N];
+    Scales scales{};
+    uint32_t rows = 0;                          // of the tile on its way, a lane each
     auto fetch = [&](const KeyPlace &at) {
+        rows = at.block * a.block_tokens + at.row_in_block;
+        if (E4M3) scales = load_scales(a, at.block, head);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const uint64_t from = __shfl(at.row, i * RP + fetched) * row_pitch + piece * 16;
+            const uint64_t from = __shfl(rows, i * RP + fetched) * row_pitch + piece * 16;
             kr[i] = *reinterpret_cast<const u32x4 *>(k_head + from);
             vr[i] = *reinterpret_cast<const u32x4 *>(v_head + from);
         }
@@ -501,11 +539,11 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_many_kernel(const AttnArgs a)
     if (threadIdx.x < 3) odd_tile[threadIdx.x] = 0;
     __syncthreads();
     const uint32_t tiles = (it.end - it.begin + KT - 1) / KT;
-    KeyPlace at{}, next{};
+    KeyPlace next{};
     if (tiles) {
-        at = find_key<E4M3>(a, it, head, it.begin + lane);
-        fetch(at);
-        next = find_key<E4M3>(a, it, head, it.begin + KT + lane);
+        const KeyPlace first = find_key(a, it, it.begin + lane);
+        next = find_key(a, it, it.begin + KT + lane);
+        fetch(first);
     }
     for (uint32_t tile = 0; tile < tiles; ++tile) {
         const uint32_t v0 = it.begin + tile * KT;
@@ -515,15 +553,16 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_many_kernel(const AttnArgs a)
             odd_tile[tile % 3] = 1;
             make_plain<T, E4M3>(vr);
         }
+        const Scales by{in_range(scales.k), in_range(scales.v)};
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const uint32_t r = i * RP + fetched;
             if (E4M3) {
                 u32x4 x, y;
-                codes_to_half<T, E4M3>(kr[i], __shfl(at.scale_k, (int)r), &x, &y);
+                codes_to_half<T, E4M3>(kr[i], __shfl(by.k, (int)r), &x, &y);
                 *reinterpret_cast<u32x4 *>(k_lds + r * RB + (((2 * piece) ^ (r & 7)) << 4)) = x;
                 *reinterpret_cast<u32x4 *>(k_lds + r * RB + (((2 * piece + 1) ^ (r & 7)) << 4)) = y;
-                codes_to_half<T, E4M3>(vr[i], __shfl(at.scale_v, (int)r), &x, &y);
+                codes_to_half<T, E4M3>(vr[i], __shfl(by.v, (int)r), &x, &y);
                 *reinterpret_cast<u32x4 *>(v_lds + r * RB + ((piece ^ (r & kSwizzle)) << 5)) = x;
                 *reinterpret_cast<u32x4 *>(v_lds + r * RB + ((piece ^ (r & kSwizzle)) << 5) + 16) = y;
             } else {
@@ -531,11 +570,10 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_many_kernel(const AttnArgs a)
                 *reinterpret_cast<u32x4 *>(v_lds + r * RB + (((piece >> 1) ^ (r & kSwizzle)) << 5) + ((piece & 1) << 4)) = vr[i];
             }
         }
-        const KeyPlace now = at;
+        const uint32_t now_rows = rows;
         if (tile + 1 < tiles) {
-            at = next;
-            fetch(at);
-            if (tile + 2 < tiles) next = find_key<E4M3>(a, it, head, v0 + 2 * KT + lane);
+            fetch(next);
+            if (tile + 2 < tiles) next = find_key(a, it, v0 + 2 * KT + lane);
         }
         __syncthreads();
         const bool odd = odd_tile[tile % 3] != 0;
@@ -573,8 +611,8 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_many_kernel(const AttnArgs a)
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-        top = fmaxf(top, __shfl_xor(top, 32)) * a.c;
-        if (__any(top > m)) {
+        top = max_halves(top) * a.c;
+        if (__any(top > m + kSlack)) {
             const float to = fmaxf(m, top), f = factor(m, to);
             m = to;
             l *= f;
@@ -609,7 +647,7 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_many_kernel(const AttnArgs a)
             }
         if (odd) {
             for (uint32_t j = 0; j < KT && v0 + j < it.end; ++j) {
-                const uint32_t pool_row = __shfl(now.row, (int)j), v = v0 + j, t = v < it.sinks ? v : v + it.gap;
+                const uint32_t pool_row = __shfl(now_rows, (int)j), v = v0 + j, t = v < it.sinks ? v : v + it.gap;
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -646,22 +684,26 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_many_kernel(const AttnArgs a)
     if (h == 0) *reinterpret_cast<f32x2 *>(to + 128 * D + 2 * i) = f32x2{m, l};
 }
 
-// Rows whose keys were cut: a wavefront a row, D / 64 elements a lane ----------------------------------------------------------------
-template <typename T, int D>
+// Rows whose keys were cut ---------------------------------------------------------------------------------------------------------
+//
+// WAVES wavefronts a row, D / 64 elements a lane: one where there are few pieces, four, a quarter of the pieces each, where there are many
+// (64 pieces for 32 rows, 8-bit step of one long request: 69 us with one and 8 pieces on their way).
+template <typename T, int D, int WAVES>
 __global__ void __launch_bounds__(256) kvl_attn_join_kernel(const AttnArgs a, const JoinItem *joins, uint32_t groups) {
-    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    constexpr int E = D / 64, ROWS = 4 / WAVES;
+    __shared__ float parts[4][64 * E + 2];
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const JoinItem it = joins[blockIdx.x / groups / a.kv_heads];
-    const uint32_t head = blockIdx.x / groups % a.kv_heads, i = blockIdx.x % groups * 4 + wave;
-    if (i >= it.n_rows) return;
+    const uint32_t head = blockIdx.x / groups % a.kv_heads, i = blockIdx.x % groups * ROWS + wave / WAVES;
+    if (i >= it.n_rows) return;                         // (all wavefronts of the row)
     const uint32_t floats = it.tile_rows * (D + 2);
     const uint64_t pitch = (uint64_t)a.kv_heads * floats;
     const float *from = a.workspace + it.partial + (uint64_t)head * floats;
-    constexpr int E = D / 64;
     float m = -__builtin_inff(), l = 0, e[2] = {0, 0};
-    for (uint32_t first = 0; first < it.pieces; first += 64) {
-        const uint32_t some = min(64u, it.pieces - first);
+    for (uint32_t first = wave % WAVES; first < it.pieces; first += 64 * WAVES) {
+        const uint32_t some = min(64u, (it.pieces - first + WAVES - 1) / WAVES);
         f32x2 state{-__builtin_inff(), 0};
-        if (lane < some) state = *reinterpret_cast<const f32x2 *>(from + (first + lane) * pitch + it.tile_rows * D + 2 * i);
+        if (lane < some) state = *reinterpret_cast<const f32x2 *>(from + (first + lane * WAVES) * pitch + it.tile_rows * D + 2 * i);
         float top = state[0];
 #pragma unroll
         for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
@@ -674,13 +716,45 @@ __global__ void __launch_bounds__(256) kvl_attn_join_kernel(const AttnArgs a, co
         e[0] *= f;
         e[1] *= f;
         const float *rows = from + first * pitch + i * D + lane * E;
-#pragma unroll 8
-        for (uint32_t k = 0; k < some; ++k) {
-            const float by = __shfl(mine, (int)k);
-            const float *at = rows + k * pitch;
-            e[0] = __builtin_fmaf(at[0], by, e[0]);
-            if (E == 2) e[1] = __builtin_fmaf(at[E - 1], by, e[1]);
+        const uint64_t step = WAVES * pitch;
+        for (uint32_t k = 0; k < some; k += 8) {
+            float x[8][2];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float *at = rows + min(k + j, some - 1) * step;
+                x[j][0] = at[0];
+                x[j][1] = at[E - 1];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float by = k + j < some ? __shfl(mine, (int)(k + j)) : 0.f;
+                e[0] = __builtin_fmaf(x[j][0], by, e[0]);
+                if (E == 2) e[1] = __builtin_fmaf(x[j][1], by, e[1]);
+            }
         }
+    }
+    if (WAVES > 1) {
+        parts[wave][lane * E] = e[0];
+        if (E == 2) parts[wave][lane * E + E - 1] = e[1];
+        if (lane == 0) {
+            parts[wave][64 * E] = m;
+            parts[wave][64 * E + 1] = l;
+        }
+        __syncthreads();
+        if (wave) return;
+        float top = m;
+        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, parts[w][64 * E]);
+        const float f = factor(m, top);
+        l *= f;
+        e[0] *= f;
+        e[1] *= f;
+        for (int w = 1; w < WAVES; ++w) {
+            const float by = factor(parts[w][64 * E], top);
+            l += by * parts[w][64 * E + 1];
+            e[0] = __builtin_fmaf(by, parts[w][lane * E], e[0]);
+            if (E == 2) e[1] = __builtin_fmaf(by, parts[w][lane * E + E - 1], e[1]);
+        }
+        m = top;
     }
     const uint32_t row = it.first_row + i, token = it.token0 + row / a.group, h = head * a.group + row % a.group;
     const float over = l == 0.f ? 0.f : 1.f / l;

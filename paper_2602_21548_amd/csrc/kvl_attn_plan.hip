@@ -7,25 +7,13 @@
 
 namespace kvl {
 
-// How the keys of a class's tiles are cut.  Each piece is one workgroup a cache head.  A piece has at least `least` keys;
-// beyond that the class's work is cut into about `pieces` of them in all, alike, so that none of the machine's places for
-// workgroups waits long for the last one.
-struct Cut {
-    uint32_t step, least, pieces;
-};
-static Cut cut_of(const kvl_attn_layout_t &l, uint32_t c) {
-    if (c == kRows128) return {kManyRowsTile, 512, 2048};
-    const uint32_t step = 4 * few_rows_tile(l.cache_dtype == KVL_E4M3, l.head_dim);     // a tile for each wavefront
-    return {step, step, 2048};
-}
-
 namespace {
 // The visible keys of some rows of one request, and the way they are numbered.
 struct Places {
     uint32_t begin, end, sinks, gap;
 };
 struct Tile {
-    uint32_t request, first_row, n_rows, cls;
+    uint32_t request, first_row, n_rows, cls;       // (cls: AttnClass)
     Places at;
 };
 }  // namespace
@@ -37,6 +25,68 @@ static Places places_of(const kvl_attn_layout_t &l, uint64_t first, uint64_t las
     if (l.window) lo = std::min(end, std::max(first, p0 + 1 > l.window ? p0 + 1 - l.window : 0));
     const uint64_t sinks = std::max(first, std::min<uint64_t>(l.sinks, lo));
     return {(uint32_t)first, (uint32_t)(sinks + end - lo), (uint32_t)sinks, (uint32_t)(lo - sinks)};
+}
+
+// How long the pieces are that the keys of a class's tiles are cut into, each one workgroup a cache head.
+//
+// A workgroup costs what `more` keys cost beside its own (finding its work, the first keys' way from memory, joining); the machine has room
+// for `slots` of them at once.  Up to that many run side by side, and the longest counts; more of them come in rounds, the last of
+// which is half empty on average; where anything is cut, the results have to be joined.  The length is the one, of a row of them, for which this
+// is least.  Whole steps are tiles for every wavefront.
+struct Machine {
+    uint32_t step, more, slots;
+};
+constexpr uint32_t kJoinKeys = 256;
+static Machine machine_of(const kvl_attn_layout_t &l, uint32_t c) {
+    if (c == kRows128) return {kManyRowsTile, 256, 512};
+    return {4 * few_rows_tile(l.head_dim), 512, l.cache_dtype == KVL_E4M3 && c == kRows16 ? 768u : 512u};
+}
+static uint64_t piece_of(const kvl_attn_layout_t &l, uint32_t c, const std::vector<Tile> &tiles) {
+    const Machine m = machine_of(l, c);
+    uint64_t longest = 0, keys = 0, n_tiles = 0;
+    for (const Tile &t : tiles) {
+        if (t.cls != c) continue;
+        const uint64_t n = t.at.end - t.at.begin;
+        longest = std::max(longest, n);
+        keys += n;
+        ++n_tiles;
+    }
+    const uint64_t whole = std::max<uint64_t>(1, (longest + m.step - 1) / m.step) * m.step;
+    uint64_t best = whole;
+    double least = 0;
+    // (with tiles enough for many rounds only those that are long beside the others are worth a cut)
+    const uint64_t from = n_tiles * l.kv_heads > 8ull * m.slots ? std::max<uint64_t>(m.step, keys / n_tiles / m.step * m.step) : m.step;
+    for (uint64_t piece = whole; piece >= from; piece = piece > m.step ? std::max<uint64_t>(m.step, piece * 7 / 8 / m.step * m.step) : 0) {
+        uint64_t count = 0, most = 0;
+        for (const Tile &t : tiles) {
+            if (t.cls != c) continue;
+            const uint64_t n = t.at.end - t.at.begin, k = std::max<uint64_t>(1, (n + piece - 1) / piece);
+            count += k;
+            most = std::max(most, (n + k - 1) / k);
+        }
+        const double rounds = (double)(count * l.kv_heads) / m.slots, mean = (double)keys / (double)count + m.more;
+        const double time = std::max((double)(most + m.more), rounds > 1 ? (rounds + 0.5) * mean : 0.0) + (count > n_tiles ? kJoinKeys : 0);
+        if (piece == whole || time < least) {
+            least = time;
+            best = piece;
+        }
+    }
+    return best;
+}
+
+// Requests of unlike numbers of rows, few each, go in one launch where their work is small beside a launch's own time (32 requests of 0.7-9 K
+// tokens, 4 heads, rows of 21 to 42: 65 us in one launch, 72 in two).
+static void merge_classes(const kvl_attn_layout_t &l, std::vector<Tile> &tiles) {
+    uint64_t keys = 0;
+    uint32_t most = 0;
+    for (const Tile &t : tiles) {
+        if (t.cls == kRows128) continue;
+        keys += t.at.end - t.at.begin;
+        most = std::max(most, t.cls);
+    }
+    if (keys * l.kv_heads > (1u << 21)) return;
+    for (Tile &t : tiles)
+        if (t.cls != kRows128) t.cls = most;
 }
 
 static int check_attn_layout(const kvl_attn_layout_t *l) {
@@ -95,27 +145,24 @@ static int build_attn(const kvl_attn_layout_t *layout, const kvl_request_t *req,
     uint64_t floats = 0;
     if (flags & KVL_GATHER) {
         std::vector<Tile> tiles;
-        uint64_t keys[kAttnClasses] = {};
         for (uint32_t r = 0; r < n_req; ++r) {
             const uint64_t hit = req[r].hit_tokens, n = req[r].append_tokens, rows = n * group;
             const uint64_t first = flags & KVL_TOKENS_APPEND ? hit : 0, last = flags & (KVL_TOKENS_APPEND | KVL_TOKENS_ALL) ? hit + n : hit;
-            const uint32_t c = rows <= 16 ? kRows16 : rows <= 32 ? kRows32 : rows <= 64 ? kRows64 : kRows128;
+            const uint32_t c = rows <= 64 ? (uint32_t)(rows - 1) / 16 : kRows128;
             for (uint64_t r0 = 0; r0 < rows; r0 += kClassRows[c]) {
                 const uint64_t r1 = std::min<uint64_t>(rows, r0 + kClassRows[c]);
                 const Places at = places_of(l, first, last, hit + r0 / group, hit + (r1 - 1) / group);
                 tiles.push_back({r, (uint32_t)r0, (uint32_t)(r1 - r0), c, at});
-                keys[c] += at.end - at.begin;
             }
         }
+        merge_classes(l, tiles);
         for (uint32_t c = 0; c < kAttnClasses; ++c) {
-            const Cut cut = cut_of(l, c);
-            const uint64_t share = (keys[c] * l.kv_heads + cut.pieces - 1) / cut.pieces;
-            const uint64_t piece = std::max<uint64_t>(cut.least, (share + cut.step - 1) / cut.step * cut.step);
+            const uint64_t piece = piece_of(l, c, tiles), step = machine_of(l, c).step;
             const size_t from = items.size();
             for (const Tile &t : tiles) {
                 if (t.cls != c) continue;
                 const uint64_t n = t.at.end - t.at.begin, pieces = std::max<uint64_t>(1, (n + piece - 1) / piece);
-                const uint64_t span = ((n + pieces - 1) / pieces + cut.step - 1) / cut.step * cut.step;
+                const uint64_t span = ((n + pieces - 1) / pieces + step - 1) / step * step;
                 const uint64_t used = std::max<uint64_t>(1, span ? (n + span - 1) / span : 1);
                 AttnItem it{(uint32_t)token0[t.request], req[t.request].hit_tokens, (uint32_t)table0[t.request], t.first_row, t.n_rows,
                             0, 0, t.at.sinks, t.at.gap, (uint32_t)used, floats};
@@ -130,6 +177,7 @@ static int build_attn(const kvl_attn_layout_t *layout, const kvl_request_t *req,
                 if (used > 1) {
                     joins.push_back({it.token0, it.first_row, it.n_rows, it.pieces, kClassRows[c], 0, floats});
                     plan->most_join_rows = std::max(plan->most_join_rows, it.n_rows);
+                    plan->most_pieces = std::max(plan->most_pieces, it.pieces);
                     floats += used * size;
                 }
             }
@@ -152,7 +200,7 @@ static int build_attn(const kvl_attn_layout_t *layout, const kvl_request_t *req,
         }
         plan->workspace_bytes = floats * sizeof(float);
         plan->n_join = (uint32_t)joins.size();
-        if ((uint64_t)plan->n_join * l.kv_heads * ((plan->most_join_rows + 3) / 4) >= (1u << 24)) return KVL_ERANGE;
+        if ((uint64_t)plan->n_join * l.kv_heads * plan->join_groups() >= (1u << 24)) return KVL_ERANGE;
     }
 
     // append: the new tokens' places, and the blocks that receive them
@@ -175,7 +223,7 @@ static int build_attn(const kvl_attn_layout_t *layout, const kvl_request_t *req,
                 const uint32_t id = (uint32_t)req[r].block_table[b], n = (uint32_t)(upto - t);
                 if (taken[id] == stamp) return KVL_EALIAS;
                 taken[id] = stamp;
-                blocks.push_back({id, (uint32_t)(token0[r] + t - hit), (uint32_t)(t - b * bs), n});
+                blocks.push_back({id, (uint32_t)(token0[r] + t - hit), (uint32_t)(t - b * bs), n, (uint32_t)t, {}});
                 plan->most_append_rows = std::max(plan->most_append_rows, n);
                 for (; t < upto; ++t) places.push_back({(uint32_t)t, (uint32_t)(id * bs + t - b * bs)});
             }
