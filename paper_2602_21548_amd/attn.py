@@ -52,6 +52,13 @@ for _name, (_res, _args) in SIGNATURES.items():
     _fn = getattr(_lib, _name)
     _fn.restype, _fn.argtypes = _res, _args
 
+if _b._native is not None:
+    _b._native.setup_attn(torch.float32, *(C.cast(getattr(_lib, f), C.c_void_p).value for f in ("kvl_append_layer", "kvl_attn_layer")))
+    # (as binding.py's: what the library returned, or 1 for a call that is the general path's)
+    _fast_append, _fast_attn = _b._native.append_layer, _b._native.attn_layer
+else:
+    _fast_append = _fast_attn = _b._not_taken
+
 
 def make_attn_layout(block_tokens: int, q_heads: int, kv_heads: int, head_dim: int, pool_blocks: int, dtype=torch.bfloat16,
                      cache_dtype=None, window: int = 0, sinks: int = 0, rope_dim: int = 0,
@@ -70,7 +77,7 @@ def make_attn_layout(block_tokens: int, q_heads: int, kv_heads: int, head_dim: i
                              rope_dim, rope_pairs, pool_blocks)
 
 
-class AttnPlan:
+class AttnPlan(_b._native.AttnPlanBase if _b._native is not None else object):
     """Owner of a kvl_attn_plan_t*."""
 
     def __init__(self, handle: int, layout: kvl_attn_layout_t, flags: int):
@@ -88,9 +95,14 @@ class AttnPlan:
         self._pointers = C.c_void_p * len(self.plane_bytes)
         self._q_shape = (self.tokens, int(layout.q_heads), int(layout.head_dim))
         self._kv_shape = (self.tokens, int(layout.kv_heads), int(layout.head_dim))
+        if _b._native is not None:
+            self._set(handle or 0, self.plane_bytes, self.dtype, self.tokens, layout.q_heads, layout.kv_heads, layout.head_dim,
+                      layout.rope_dim // 2, 1 / math.sqrt(layout.head_dim))
 
     def destroy(self) -> None:
         if self._h:
+            if _b._native is not None:
+                self._clear()
             _lib.kvl_attn_plan_destroy(self._h)
             self._h = C.c_void_p(None)
 
@@ -169,6 +181,9 @@ def kvl_append_layer(plan: AttnPlan, k: torch.Tensor, v: torch.Tensor, pool_plan
     projection's output).  rope: float32 [positions, rope_dim / 2, 2], cosines and sines.  An 8-bit pool has four planes: codes
     of keys and of values, float32 [pool_blocks, kv_heads] scales of each."""
     what = "kvl_append_layer"
+    rc = _fast_append(plan, k, v, pool_planes, rope, q, q_out, stream)
+    if rc <= 0:
+        return _b._check(rc, what)
     a = kvl_append_t()
     arr = _planes(plan, pool_planes, what)
     a.k, a.k_stride = _rows(plan, k, plan._kv_shape, f"{what} k")
@@ -199,6 +214,9 @@ def kvl_attn_layer(plan: AttnPlan, q: torch.Tensor, pool_planes: Sequence[torch.
     [tokens, q_heads], or None; workspace: a device tensor of plan.workspace_bytes (None if that is 0), in nobody else's use
     until the work is done."""
     what = "kvl_attn_layer"
+    rc = _fast_attn(plan, q, pool_planes, out, workspace, scale, lse, stream)
+    if rc <= 0:
+        return _b._check(rc, what)
     a = kvl_attn_t()
     arr = _planes(plan, pool_planes, what)
     a.q, a.q_stride = _rows(plan, q, plan._q_shape, f"{what} q")

@@ -203,6 +203,10 @@ _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _current_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
+def _not_taken(*_args):
+    return 1
+
+
 if _native is not None and _current_raw_stream is not None and _current_device is not None:
     _native.setup(torch.Tensor, np.ndarray, _current_raw_stream, _current_device, torch.cuda.is_initialized,
                   *(C.cast(getattr(_lib, f), C.c_void_p).value
@@ -214,10 +218,6 @@ if _native is not None and _current_raw_stream is not None and _current_device i
     _fast_to_pool, _fast_to_blocks = _native.fullblocks_to_pool_layer, _native.pool_to_fullblocks_layer
 else:
     _native = None
-
-    def _not_taken(*_args):
-        return 1
-
     _fast_pack = _fast_unpack = _fast_move = _fast_to_pool = _fast_to_blocks = _not_taken
 
 
