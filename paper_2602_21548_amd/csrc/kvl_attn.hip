@@ -17,10 +17,9 @@ static void launch_attn(const kvl_attn_plan_t *plan, AttnArgs a, AttnLaunch &go)
         a.items = items + plan->class_first[c];
         const uint32_t groups = n * a.kv_heads;
         const bool last = --left == 0;
-        if (c == kRows16) go(last, kvl_attn_few_kernel<T, E4M3, D, 1>, groups, 256, a);
-        else if (c == kRows32) go(last, kvl_attn_few_kernel<T, E4M3, D, 2>, groups, 256, a);
-        else if (c == kRows48) go(last, kvl_attn_few_kernel<T, E4M3, D, 3>, groups, 256, a);
-        else if (c == kRows64) go(last, kvl_attn_few_kernel<T, E4M3, D, 4>, groups, 256, a);
+        if (c == kRows16) go(last, kvl_attn_few_kernel<T, E4M3, D, 1, 1>, groups, 256, a);
+        else if (c == kRows32) go(last, kvl_attn_few_kernel<T, E4M3, D, 2, 1>, groups, 256, a);
+        else if (c == kRows64) go(last, kvl_attn_few_kernel<T, E4M3, D, 2, 2>, groups, 256, a);
         else go(last, kvl_attn_many_kernel<T, E4M3, D>, groups, 256, a);
     }
     if (plan->n_join) {

@@ -9,8 +9,8 @@
 namespace kvl {
 
 // Which kernel takes a request's rows (new tokens times the query heads that share a cache head), and in tiles of how many.
-enum AttnClass : uint32_t { kRows16 = 0, kRows32, kRows48, kRows64, kRows128, kAttnClasses };
-constexpr uint32_t kClassRows[kAttnClasses] = {16, 32, 48, 64, 128};
+enum AttnClass : uint32_t { kRows16 = 0, kRows32, kRows64, kRows128, kAttnClasses };
+constexpr uint32_t kClassRows[kAttnClasses] = {16, 32, 64, 128};
 
 // One piece of work of the attention kernels, for every cache head (kvl_attn_item_t, with what a kernel would have to look up).
 struct AttnItem {

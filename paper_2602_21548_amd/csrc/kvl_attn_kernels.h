@@ -101,14 +101,22 @@ __device__ __forceinline__ Scales load_scales(const AttnArgs &a, uint32_t block,
 }
 __device__ __forceinline__ float in_range(float scale) { return fminf(fmaxf(scale, kLowestScale), kHighestScale); }
 
-__device__ __forceinline__ bool sees(const AttnArgs &a, uint32_t position, uint32_t t) {
-    return t <= position && (t + a.window > position || t < a.sinks);
-}
-
 // Whether every query at positions [p0, p1] sees every key at places [v0, v1].
 __device__ __forceinline__ bool all_seen(const AttnArgs &a, const AttnItem &it, uint32_t v0, uint32_t v1, uint32_t p0, uint32_t p1) {
     const uint32_t t0 = v0 < it.sinks ? v0 : v0 + it.gap, t1 = v1 < it.sinks ? v1 : v1 + it.gap;
     return v1 < it.end && t1 <= p0 && (t0 + a.window > p1 || t1 < a.sinks);
+}
+
+// The places that a query at `position` sees among those before `end`: v - first < count, and v < sinks.  (The first place whose token is t or a later
+// one: t up to the first tokens' end, and t - gap beyond the gap.)
+struct Seen {
+    uint32_t first, count, sinks;
+    __device__ __forceinline__ bool operator()(uint32_t v) const { return (v - first < count) | (v < sinks); }
+};
+__device__ __forceinline__ Seen seen_from(const AttnArgs &a, const AttnItem &it, uint32_t position) {
+    auto place = [&](uint32_t t) { return t <= it.sinks ? t : max(t, it.sinks + it.gap) - it.gap; };
+    const uint32_t end = min(place(position + 1), it.end), first = place(position + 1 > a.window ? position + 1 - a.window : 0);
+    return {first, end > first ? end - first : 0, min(place(a.sinks), end)};
 }
 
 // Whether some of the elements in a word, two of T or four codes, are infinite or NaN; and the word with zeros for them.
@@ -189,14 +197,18 @@ __device__ __forceinline__ void write_lse(const AttnArgs &a, uint32_t token0, ui
 
 // Few rows -------------------------------------------------------------------------------------------------------------------------
 //
-// Up to 16 * RT rows against pieces of their keys.  The keys' and values' bytes bound it: each is read once, by one wavefront, and used
+// Up to 16 * RT * HALVES rows against pieces of their keys.  The keys' and values' bytes bound it: each is read once, by one wavefront, and used
 // for all rows.  The wavefronts of a workgroup take tiles of keys in turn, each with its own maximum, sum and outputs, without a
 // barrier until the end, so that at any time all but the tile in work is on its way; then they are joined in the LDS.  K goes from memory
 // to the registers of the matrix instructions as it lies: lane (n, g) has key n's elements of four-lane group g, and the queries are laid out
 // to match.  V goes through the wavefront's own part of the LDS, which turns it.  8-bit codes become T there and here, exactly; their
 // scales multiply scores (K) and join the exponent (V: with x = c s_k <q, K_t> + log2 s_v, 2^(x - m) multiplies the codes, and 2^(x - m) / s_v
 // is the term of l), in 32 bits, whatever T is.
-template <typename T, bool E4M3, int D, int RT>
+//
+// Beyond 32 rows the registers do not hold a wavefront's outputs beside what is on its way, and scratch memory's loads come in order behind those of
+// the next keys: there HALVES = 2, and two wavefronts take the same tile of keys, half of the rows each; what the second one loads is in the caches.
+// (32 requests of 21 to 42 rows, 8-bit heads of 128: 59 us with three tiles of rows a wavefront and five such loads for each of keys, 51 so.)
+template <typename T, bool E4M3, int D, int RT, int HALVES>
 __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) {
     constexpr int KT = few_rows_tile(D), NB = KT / 16;        // keys of a tile, blocks of 16
     constexpr int RB = D * (E4M3 ? 1 : 2);                          // bytes of a row
@@ -211,12 +223,18 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
     __shared__ __attribute__((aligned(16))) char lds[kBytes];
     __shared__ f32x2 state[4][RT * 16];
     typedef typename T::x8 x8;
-    __shared__ x8 staged[RT > 1 ? RT * CH : 1][64];
+    // where there are several tiles of rows: queries, in the order in which the matrix instructions take them, and what each row sees
+    constexpr bool kStaged = RT > 1;
+    constexpr int kTiles = RT * HALVES;
+    __shared__ x8 staged[kStaged ? kTiles * CH : 1][64];
+    __shared__ Seen seen_of[kStaged ? kTiles * 16 : 1];
 
     uint32_t item, head;
     place_of<(RB < 256)>(blockIdx.x, gridDim.x, a.kv_heads, &item, &head);
     const AttnItem it = a.items[item];
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 16, g = lane / 16;
+    constexpr uint32_t kStreams = 4 / HALVES;
+    const uint32_t half = wave % HALVES, stream = wave / HALVES, first_tile = half * RT;
     char *mine = lds + wave * kWaveBytes;
     float *key_c = reinterpret_cast<float *>(mine + KT * RB), *key_log = key_c + KT, *key_over = key_log + KT;
     const uint64_t row_pitch = (uint64_t)a.kv_heads * RB;
@@ -250,20 +268,16 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
 
     const uint32_t tiles = (it.end - it.begin + KT - 1) / KT;
     KeyPlace next{};
-    if (wave < tiles) {
-        const KeyPlace first = find_key(a, it, it.begin + wave * KT + lane % KT);
-        next = find_key(a, it, it.begin + (wave + 4) * KT + lane % KT);
+    if (stream < tiles) {
+        const KeyPlace first = find_key(a, it, it.begin + stream * KT + lane % KT);
+        next = find_key(a, it, it.begin + (stream + kStreams) * KT + lane % KT);
         fetch(first);
     }
-    // Queries: in registers for 16 rows, else in the LDS, in the order in which the matrix instructions take them.
-    constexpr bool kStaged = RT > 1;
     x8 q[kStaged ? 1 : CH];
-    uint32_t position[RT];
     const uint32_t p0 = it.hit + it.first_row / a.group, p1 = it.hit + (it.first_row + it.n_rows - 1) / a.group;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
+    for (int r = 0; r < kTiles; ++r) {
         const uint32_t i = min(r * 16 + n, it.n_rows - 1), row = it.first_row + i, token = row / a.group;
-        position[r] = it.hit + token;
         const char *from = a.q + 2 * ((it.token0 + token) * a.q_stride + (head * a.group + row % a.group) * D);
 #pragma unroll
         for (int s = 0; s < CH; ++s) {
@@ -272,8 +286,12 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
             else if (wave == (uint32_t)(r * CH + s) % 4) staged[r * CH + s][lane] = *reinterpret_cast<const x8 *>(from + 2 * dim);
         }
     }
+    auto seen_by = [&](uint32_t i) { return seen_from(a, it, it.hit + (it.first_row + min(i, it.n_rows - 1)) / a.group); };
+    Seen seen_here{};
+    if (!kStaged) seen_here = seen_by(n);
+    else if (threadIdx.x < kTiles * 16) seen_of[threadIdx.x] = seen_by(threadIdx.x);
     if (kStaged) __syncthreads();
-    for (uint32_t tile = wave; tile < tiles; tile += 4) {
+    for (uint32_t tile = stream; tile < tiles; tile += kStreams) {
         const uint32_t v0 = it.begin + tile * KT;
         const bool whole = all_seen(a, it, v0, v0 + KT - 1, p0, p1);
         // Values that only some of the rows see must not reach the others: 0 * inf is NaN.  Infinities and NaN of such a tile are added
@@ -291,7 +309,7 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
                 const float by = in_range(scales.v);
                 key_c[lane] = a.c * in_range(scales.k);
                 key_log[lane] = __log2f(by);
-                key_over[lane] = 1.f / by;
+                key_over[lane] = __builtin_amdgcn_rcpf(by);        // (to a unit in the last place of 32 bits, as the sum it goes into)
             }
         }
         __builtin_amdgcn_wave_barrier();
@@ -301,19 +319,20 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
 #pragma unroll
             for (int i = 0; i < KP; ++i) kr[b][i] = kn[b][i];
         // the next tile comes while this one is worked on
-        if (tile + 4 < tiles) {
+        if (tile + kStreams < tiles) {
             fetch(next);
-            if (tile + 8 < tiles) next = find_key(a, it, it.begin + (tile + 8) * KT + lane % KT);
+            if (tile + 2 * kStreams < tiles) next = find_key(a, it, it.begin + (tile + 2 * kStreams) * KT + lane % KT);
         }
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
+            if (HALVES > 1 && (first_tile + r) * 16 >= it.n_rows) continue;
             // scores: lane (n, g) gets row n's of keys 16 b + 4 g + i
             f32x4 s[NB];
 #pragma unroll
             for (int b = 0; b < NB; ++b) s[b] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
-                const x8 x = kStaged ? staged[r * CH + j][lane] : q[kStaged ? 0 : j];
+                const x8 x = kStaged ? staged[(first_tile + r) * CH + j][lane] : q[kStaged ? 0 : j];
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
                     x8 k;
@@ -337,13 +356,20 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     s[b][i] = E4M3 ? __builtin_fmaf(s[b][i], kc[i], kl[i]) : s[b][i] * kc[i];
-                    if (!whole) {
-                        const uint32_t v = v0 + at_key + i, t = v < it.sinks ? v : v + it.gap;
-                        if (v >= it.end || !sees(a, position[r], t)) s[b][i] = -__builtin_inff();
-                    }
-                    top = fmaxf(top, s[b][i]);
                 }
             }
+            if (!whole) {
+                const Seen seen = kStaged ? seen_of[(first_tile + r) * 16 + n] : seen_here;
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!seen(v0 + 16 * b + 4 * g + i)) s[b][i] = -__builtin_inff();
+            }
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[b][i]);
             top = max_quarters(top);
             if (__any(top > m[r] + kSlack)) {
                 const float to = fmaxf(m[r], top), f = factor(m[r], to);
@@ -389,17 +415,16 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
                     }
                     o[r][d] = T::mma16(__builtin_bit_cast(x8, w), p[u], o[r][d]);
                 }
-            if (RT > 2) __builtin_amdgcn_sched_barrier(0);      // (one row tile's scores at a time in the registers)
-        }
+                    }
         if (odd) {
             for (uint32_t j = 0; j < KT && v0 + j < it.end; ++j) {
-                const uint32_t row = __shfl(now_rows, (int)j), v = v0 + j, t = v < it.sinks ? v : v + it.gap;
+                const uint32_t row = __shfl(now_rows, (int)j);
 #pragma unroll
                 for (int d = 0; d < DC; ++d) {
                     const f32x4 e = odd_values<T, E4M3, D>(a, head, row, 16 * d + 4 * g);
 #pragma unroll
                     for (int r = 0; r < RT; ++r)
-                        if (sees(a, position[r], t)) o[r][d] += e;
+                        if ((kStaged ? seen_of[(first_tile + r) * 16 + n] : seen_here)(v0 + j)) o[r][d] += e;
                 }
             }
         }
@@ -421,29 +446,33 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
     for (int r = 0; r < RT; ++r) {
         __syncthreads();                        // (nobody reads V, or the rows before, any more; the states are there)
         float top = -__builtin_inff();
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, state[w][r * 16 + n][0]);
+        for (uint32_t w = half; w < 4; w += HALVES) top = fmaxf(top, state[w][r * 16 + n][0]);
         const float f = factor(m[r], top);
 #pragma unroll
         for (int d = 0; d < DC; ++d) *reinterpret_cast<f32x4 *>(sums + (wave * 16 + n) * OS + 16 * d + 4 * g) = o[r][d] * f;
         __syncthreads();
-        const uint32_t i = r * 16 + row;
-        if (i >= it.n_rows) continue;
-        float most = -__builtin_inff(), sum = 0, e[E] = {};
-        for (int w = 0; w < 4; ++w) most = fmaxf(most, state[w][i][0]);
-        for (int w = 0; w < 4; ++w) {
-            sum += state[w][i][1] * factor(state[w][i][0], most);
 #pragma unroll
-            for (int j = 0; j < E; ++j) e[j] += sums[(w * 16 + row) * OS + dim + j];
-        }
-        if (it.pieces == 1) {
-            write_row<T, E>(a, it.token0, it.first_row + i, head, dim, D, sum, e);
-            if (dim == 0) write_lse<T>(a, it.token0, it.first_row + i, head, most, sum);
-        } else {
-            constexpr uint32_t kFloats = RT * 16 * (D + 2);
-            float *to = a.workspace + it.partial + (uint64_t)head * kFloats;
+        for (uint32_t hh = 0; hh < HALVES; ++hh) {
+            const uint32_t i = (hh * RT + r) * 16 + row;
+            if (i >= it.n_rows) continue;
+            float most = -__builtin_inff(), sum = 0, e[E] = {};
+            for (uint32_t w = hh; w < 4; w += HALVES) most = fmaxf(most, state[w][r * 16 + row][0]);
+            for (uint32_t w = hh; w < 4; w += HALVES) {
+                const f32x2 at = state[w][r * 16 + row];
+                sum += at[1] * factor(at[0], most);
 #pragma unroll
-            for (int j = 0; j < E; ++j) to[i * D + dim + j] = e[j];
-            if (dim == 0) *reinterpret_cast<f32x2 *>(to + RT * 16 * D + 2 * i) = f32x2{most, sum};
+                for (int j = 0; j < E; ++j) e[j] += sums[(w * 16 + row) * OS + dim + j];
+            }
+            if (it.pieces == 1) {
+                write_row<T, E>(a, it.token0, it.first_row + i, head, dim, D, sum, e);
+                if (dim == 0) write_lse<T>(a, it.token0, it.first_row + i, head, most, sum);
+            } else {
+                constexpr uint32_t kFloats = kTiles * 16 * (D + 2);
+                float *to = a.workspace + it.partial + (uint64_t)head * kFloats;
+#pragma unroll
+                for (int j = 0; j < E; ++j) to[i * D + dim + j] = e[j];
+                if (dim == 0) *reinterpret_cast<f32x2 *>(to + kTiles * 16 * D + 2 * i) = f32x2{most, sum};
+            }
         }
     }
 }
@@ -490,8 +519,11 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
     constexpr int RP = 256 / PR;                                    // rows that the workgroup fetches at once
     constexpr int N = KT / RP;                                      // a lane's pieces of a tile
     constexpr int CH = D / 16, DB = D / 32;                         // steps of the first product; blocks of the output
-    constexpr int kSwizzle = D / 16 - 1;
     static_assert(KT % RP == 0 && KT == 64, "whole pieces; a key a lane");
+    // Pieces of 16 bytes are turned by their row's number so that the 16 rows that lanes read of K together, and the 4 rows by 64 bytes of V, lie in
+    // different banks (256 bytes of them): rows of 128 bytes take half of these each.
+    auto k_turn = [](uint32_t r) { return D == 128 ? r & 15 : r >> 1 & 7; };
+    auto v_turn = [](uint32_t r) { return D == 128 ? (r & 3) << 2 | (r & 1) : (r >> 1 & 1) * 5; };
     __shared__ __attribute__((aligned(16))) char lds[2][2][KT * RB];
     __shared__ uint32_t odd_tile[3];
     typedef typename T::x8 x8;
@@ -506,10 +538,10 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
     const uint32_t rows_before = wave * 32;
     const bool works = rows_before < it.n_rows;
     const uint32_t row = it.first_row + min(rows_before + n, it.n_rows - 1);
-    const uint32_t position = it.hit + row / a.group;
     const uint32_t p0 = it.hit + it.first_row / a.group, p1 = it.hit + (it.first_row + it.n_rows - 1) / a.group;
     const uint32_t w0 = it.hit + (it.first_row + min(rows_before, it.n_rows - 1)) / a.group,
                    w1 = it.hit + (it.first_row + min(rows_before + 31, it.n_rows - 1)) / a.group;
+    const Seen seen = seen_from(a, it, it.hit + row / a.group);
     x8 q[CH];
     {
         const char *from = a.q + 2 * ((it.token0 + row / a.group) * a.q_stride + (head * a.group + row % a.group) * D);
@@ -560,14 +592,14 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
             if (E4M3) {
                 u32x4 x, y;
                 codes_to_half<T, E4M3>(kr[i], __shfl(by.k, (int)r), &x, &y);
-                *reinterpret_cast<u32x4 *>(k_lds + r * RB + (((2 * piece) ^ (r & 7)) << 4)) = x;
-                *reinterpret_cast<u32x4 *>(k_lds + r * RB + (((2 * piece + 1) ^ (r & 7)) << 4)) = y;
+                *reinterpret_cast<u32x4 *>(k_lds + r * RB + (((2 * piece) ^ k_turn(r)) << 4)) = x;
+                *reinterpret_cast<u32x4 *>(k_lds + r * RB + (((2 * piece + 1) ^ k_turn(r)) << 4)) = y;
                 codes_to_half<T, E4M3>(vr[i], __shfl(by.v, (int)r), &x, &y);
-                *reinterpret_cast<u32x4 *>(v_lds + r * RB + ((piece ^ (r & kSwizzle)) << 5)) = x;
-                *reinterpret_cast<u32x4 *>(v_lds + r * RB + ((piece ^ (r & kSwizzle)) << 5) + 16) = y;
+                *reinterpret_cast<u32x4 *>(v_lds + r * RB + (((2 * piece) ^ v_turn(r)) << 4)) = x;
+                *reinterpret_cast<u32x4 *>(v_lds + r * RB + (((2 * piece + 1) ^ v_turn(r)) << 4)) = y;
             } else {
-                *reinterpret_cast<u32x4 *>(k_lds + r * RB + ((piece ^ (r & 7)) << 4)) = kr[i];
-                *reinterpret_cast<u32x4 *>(v_lds + r * RB + (((piece >> 1) ^ (r & kSwizzle)) << 5) + ((piece & 1) << 4)) = vr[i];
+                *reinterpret_cast<u32x4 *>(k_lds + r * RB + ((piece ^ k_turn(r)) << 4)) = kr[i];
+                *reinterpret_cast<u32x4 *>(v_lds + r * RB + ((piece ^ v_turn(r)) << 4)) = vr[i];
             }
         }
         const uint32_t now_rows = rows;
@@ -593,7 +625,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
             for (int i = 0; i < 16; ++i) s[b][i] = 0;
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
-                const x8 k = *reinterpret_cast<const x8 *>(k_lds + (32 * b + n) * RB + (((2 * j + h) ^ (n & 7)) << 4));
+                const x8 k = *reinterpret_cast<const x8 *>(k_lds + (32 * b + n) * RB + (((2 * j + h) ^ k_turn(n)) << 4));
                 s[b] = T::mma32(k, q[j], s[b]);
             }
         }
@@ -602,8 +634,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const uint32_t v = v0 + 32 * b + 8 * (i / 4) + 4 * h + i % 4, t = v < it.sinks ? v : v + it.gap;
-                    if (v >= it.end || !sees(a, position, t)) s[b][i] = -__builtin_inff();
+                    if (!seen(v0 + 4 * h + 32 * b + 8 * (i / 4) + i % 4)) s[b][i] = -__builtin_inff();
                 }
         }
         float top = s[0][0];
@@ -640,20 +671,20 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
         for (int u = 0; u < 4; ++u)
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
-                const uint32_t r = 16 * u + 4 * h + lane % 16 / 4, chunk = 2 * d + lane / 16 % 2;
-                const u32x2 x = read_columns16(v_lds + r * RB + ((chunk ^ (r & kSwizzle)) << 5) + (lane & 3) * 8);
-                const u32x2 y = read_columns16(v_lds + (r + 8) * RB + ((chunk ^ ((r + 8) & kSwizzle)) << 5) + (lane & 3) * 8);
+                const uint32_t r = 16 * u + 4 * h + lane % 16 / 4, at = 4 * d + 2 * (lane / 16 % 2) + lane % 4 / 2;
+                const u32x2 x = read_columns16(v_lds + r * RB + ((at ^ v_turn(r)) << 4) + lane % 2 * 8);
+                const u32x2 y = read_columns16(v_lds + (r + 8) * RB + ((at ^ v_turn(r + 8)) << 4) + lane % 2 * 8);
                 o[d] = T::mma32(__builtin_bit_cast(x8, (u32x4{x[0], x[1], y[0], y[1]})), p[u], o[d]);
             }
         if (odd) {
             for (uint32_t j = 0; j < KT && v0 + j < it.end; ++j) {
-                const uint32_t pool_row = __shfl(now_rows, (int)j), v = v0 + j, t = v < it.sinks ? v : v + it.gap;
+                const uint32_t pool_row = __shfl(now_rows, (int)j);
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
 #pragma unroll
                     for (int i = 0; i < 16; i += 4) {
                         const f32x4 e = odd_values<T, E4M3, D>(a, head, pool_row, 32 * d + 2 * i + 4 * h);
-                        if (sees(a, position, t))
+                        if (seen(v0 + j))
 #pragma unroll
                             for (int x = 0; x < 4; ++x) o[d][i + x] += e[x];
                     }

@@ -39,7 +39,7 @@ struct Machine {
 constexpr uint32_t kJoinKeys = 256;
 static Machine machine_of(const kvl_attn_layout_t &l, uint32_t c) {
     if (c == kRows128) return {kManyRowsTile, 256, 512};
-    return {4 * few_rows_tile(l.head_dim), 512, l.cache_dtype == KVL_E4M3 && c == kRows16 ? 768u : 512u};
+    return {(c == kRows64 ? 2 : 4) * few_rows_tile(l.head_dim), 512, l.cache_dtype == KVL_E4M3 && c == kRows16 ? 768u : 512u};
 }
 static uint64_t piece_of(const kvl_attn_layout_t &l, uint32_t c, const std::vector<Tile> &tiles) {
     const Machine m = machine_of(l, c);
@@ -148,7 +148,7 @@ static int build_attn(const kvl_attn_layout_t *layout, const kvl_request_t *req,
         for (uint32_t r = 0; r < n_req; ++r) {
             const uint64_t hit = req[r].hit_tokens, n = req[r].append_tokens, rows = n * group;
             const uint64_t first = flags & KVL_TOKENS_APPEND ? hit : 0, last = flags & (KVL_TOKENS_APPEND | KVL_TOKENS_ALL) ? hit + n : hit;
-            const uint32_t c = rows <= 64 ? (uint32_t)(rows - 1) / 16 : kRows128;
+            const uint32_t c = rows <= 16 ? kRows16 : rows <= 32 ? kRows32 : rows <= 64 ? kRows64 : kRows128;
             for (uint64_t r0 = 0; r0 < rows; r0 += kClassRows[c]) {
                 const uint64_t r1 = std::min<uint64_t>(rows, r0 + kClassRows[c]);
                 const Places at = places_of(l, first, last, hit + r0 / group, hit + (r1 - 1) / group);
