@@ -51,6 +51,19 @@ __device__ __forceinline__ void widen16(u32x4 x, u32x4 y, W (&e)[16]) {
     }
 }
 
+template <int AT, typename W>
+__device__ __forceinline__ void turn_neighbours(W (&e)[16], const float *row, uint32_t first, bool turns) {
+    if (!turns) return;
+    const f32x4 *from = reinterpret_cast<const f32x4 *>(row + first);
+    const f32x4 t[2] = {from[0], from[1]};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const W c = t[j / 2][j % 2 * 2], s = t[j / 2][j % 2 * 2 + 1], a = e[AT + 2 * j], b = e[AT + 2 * j + 1];
+        e[AT + 2 * j] = a * c - b * s;
+        e[AT + 2 * j + 1] = b * c + a * s;
+    }
+}
+
 // Pieces turned by the angles of table row `position`.
 template <typename W>
 __device__ __forceinline__ void turn(W (&e)[16], const float *rope, uint32_t position, const Pieces &at, uint32_t rope_dim, uint32_t pairs) {
@@ -66,20 +79,11 @@ __device__ __forceinline__ void turn(W (&e)[16], const float *rope, uint32_t pos
             e[j] = a * c - b * s;
             e[8 + j] = b * c + a * s;
         }
+        asm volatile("");       // (else the two ways' last stores become one, at an index that is not known, and `e` goes to memory)
         return;
     }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        if (!(h ? at.turn_second : at.turn_first)) continue;
-        const f32x4 *from = reinterpret_cast<const f32x4 *>(row + (h ? at.second : at.first));
-        const f32x4 t[2] = {from[0], from[1]};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const W c = t[j / 2][j % 2 * 2], s = t[j / 2][j % 2 * 2 + 1], a = e[8 * h + 2 * j], b = e[8 * h + 2 * j + 1];
-            e[8 * h + 2 * j] = a * c - b * s;
-            e[8 * h + 2 * j + 1] = b * c + a * s;
-        }
-    }
+    turn_neighbours<0>(e, row, at.first, at.turn_first);
+    turn_neighbours<8>(e, row, at.second, at.turn_second);
 }
 
 template <typename T>
@@ -137,29 +141,34 @@ __global__ void __launch_bounds__(256) kvl_append_half_kernel(const AppendArgs a
     append_half<T, D>(a, (uint64_t)blockIdx.x * blockDim.x + threadIdx.x);
 }
 
-// A double as a float rounded to odd: a later rounding to fewer bits then sees which side of a tie, or of a border, it was on.
+constexpr uint32_t kInfinity = 0x7f800000u;
+
+// A double as a float rounded to odd (cut off, with the last bit set where anything was lost): a later rounding to fewer bits then sees which side of
+// a tie, or of a border, it was on.  Below the normal floats 0, above the largest that, what is not finite infinite.  By integers: comparisons in 64 bits
+// and their branches took half of the time of the kernel below.
 __device__ __forceinline__ float to_odd(double x) {
-    const float f = (float)x;
-    const double rest = x - (double)f;
-    const uint32_t bits = __float_as_uint(f);
-    return rest != 0 && !(bits & 1u) && fabsf(f) >= 0x1p-120f && fabsf(f) < __builtin_inff() ? __uint_as_float((rest > 0) == (f > 0) ? bits + 1 : bits - 1) : f;
+    const uint64_t bits = __builtin_bit_cast(uint64_t, x);
+    const uint32_t top = (uint32_t)(bits >> 32), size = top & 0x7fffffffu;
+    uint32_t f = (((uint32_t)(bits >> 29) - (896u << 23)) & 0x7fffffffu) | min((uint32_t)bits & 0x1fffffffu, 1u);
+    f = size < 897u << 20 ? 0 : f;
+    f = size >= 1151u << 20 ? (size >= 2047u << 20 ? kInfinity : kInfinity - 1) : f;
+    return __uint_as_float(f | (top & 0x80000000u));
 }
 
 // Four codes of e4m3: x / scale to the nearest, where x may have been rounded to odd.  `over` is 1 / scale if that is a power of two (the product
-// is exact then), else 0.
-__device__ __forceinline__ uint32_t codes4(const float *x, float scale, float over) {
+// is exact then), else 0.  `odd`: not all of x need be finite.
+__device__ __forceinline__ uint32_t codes4(const float *x, float scale, float over, bool odd) {
     float f[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[i] = over != 0 ? x[i] * over : to_odd((double)x[i] / (double)scale);
-        f[i] = fminf(fmaxf(f[i], -448.f), 448.f);
-    }
+    for (int i = 0; i < 4; ++i) f[i] = __builtin_amdgcn_fmed3f(over != 0 ? x[i] * over : to_odd((double)x[i] / (double)scale), -448.f, 448.f);
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
     w = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], w, true);
     uint32_t u = (uint32_t)w;
+    if (odd) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (!(fabsf(x[i]) < __builtin_inff())) u |= 0x7fu << (8 * i);
+        for (int i = 0; i < 4; ++i)
+            if ((__float_as_uint(x[i]) & 0x7fffffffu) >= kInfinity) u |= 0x7fu << (8 * i);
+    }
     return u;
 }
 
@@ -207,19 +216,31 @@ __device__ __forceinline__ void append_codes(const AppendArgs &a, const AppendBl
 #pragma unroll
         for (int j = 0; j < 16; ++j) e[j] = to_odd(d[j]);
     };
-    auto largest = [](const float (&e)[16], float most) {
+    // the largest of the finite ones; whether all are finite (sizes of floats compare as their bits do)
+    auto largest = [](const float (&e)[16], float most, bool *odd) {
+        uint32_t size = 0;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) most = fabsf(e[j]) < __builtin_inff() ? fmaxf(most, fabsf(e[j])) : most;
-        return most;
+        for (int j = 0; j < 16; ++j) size = max(size, __float_as_uint(e[j]) & 0x7fffffffu);
+        *odd = size >= kInfinity;
+        if (*odd) {
+            size = 0;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const uint32_t x = __float_as_uint(e[j]) & 0x7fffffffu;
+                size = max(size, x < kInfinity ? x : 0u);
+            }
+        }
+        return fmaxf(most, __uint_as_float(size));
     };
-    auto store = [&](const CodesPlane &plane, uint32_t i, const float (&e)[16], float scale, float over) {
+    auto store = [&](const CodesPlane &plane, uint32_t i, const float (&e)[16], float scale, float over, bool odd) {
         const Pieces at = pieces_of<D>(i % kHeadTasks, a.rope_dim, a.rope_pairs, !plane.value);
         char *to = plane.pool + (b.row + i / kHeadTasks) * row_bytes;
-        *reinterpret_cast<u32x2 *>(to + at.first) = u32x2{codes4(e, scale, over), codes4(e + 4, scale, over)};
-        *reinterpret_cast<u32x2 *>(to + at.second) = u32x2{codes4(e + 8, scale, over), codes4(e + 12, scale, over)};
+        *reinterpret_cast<u32x2 *>(to + at.first) = u32x2{codes4(e, scale, over, odd), codes4(e + 4, scale, over, odd)};
+        *reinterpret_cast<u32x2 *>(to + at.second) = u32x2{codes4(e + 8, scale, over, odd), codes4(e + 12, scale, over, odd)};
     };
 
     float e[2][N][16], most[2] = {0, 0};
+    bool odd[2][N] = {};
 #pragma unroll
     for (int j = 0; j < N; ++j)
 #pragma unroll
@@ -227,13 +248,14 @@ __device__ __forceinline__ void append_codes(const AppendArgs &a, const AppendBl
             const uint32_t i = threadIdx.x + j * per;
             if (i >= n) continue;
             load(planes[x], i, e[x][j]);
-            most[x] = largest(e[x][j], most[x]);
+            most[x] = largest(e[x][j], most[x], &odd[x][j]);
         }
     for (uint32_t i = threadIdx.x + N * per; i < n; i += per)
         for (int x = 0; x < 2; ++x) {
             float w[16];
+            bool any;
             load(planes[x], i, w);
-            most[x] = largest(w, most[x]);
+            most[x] = largest(w, most[x], &any);
         }
 #pragma unroll
     for (int x = 32; x; x >>= 1) {
@@ -261,7 +283,7 @@ __device__ __forceinline__ void append_codes(const AppendArgs &a, const AppendBl
                 for (int j = 0; j < 4; ++j) {
                     const f32x2 c = widen_codes<0>(w[j]), d = widen_codes<1>(w[j]);
                     const float was[4] = {to_odd((double)c[0] * old[x]), to_odd((double)c[1] * old[x]), to_odd((double)d[0] * old[x]), to_odd((double)d[1] * old[x])};
-                    w[j] = codes4(was, scale, over);
+                    w[j] = codes4(was, scale, over, true);
                 }
                 *at = w;
             }
@@ -269,12 +291,12 @@ __device__ __forceinline__ void append_codes(const AppendArgs &a, const AppendBl
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const uint32_t i = threadIdx.x + j * per;
-            if (i < n) store(plane, i, e[x][j], scale, over);
+            if (i < n) store(plane, i, e[x][j], scale, over, odd[x][j]);
         }
         for (uint32_t i = threadIdx.x + N * per; i < n; i += per) {
             float w[16];
             load(plane, i, w);
-            store(plane, i, w, scale, over);
+            store(plane, i, w, scale, over, true);
         }
         if (threadIdx.x == 0) *plane.scale = scale;
     }
@@ -282,15 +304,20 @@ __device__ __forceinline__ void append_codes(const AppendArgs &a, const AppendBl
 
 // 8-bit caches: a workgroup for each block that receives rows and each head, and after those workgroups for the queries.
 template <typename T, int D>
-__global__ void __launch_bounds__(256) kvl_append_codes_kernel(const AppendArgs a) {
+__global__ void __launch_bounds__(256, 3) kvl_append_codes_kernel(const AppendArgs a) {
     __shared__ f32x2 most_of_wave[4];
     const uint32_t work = a.n_blocks * a.kv_heads;
     if (blockIdx.x >= work) {
         append_half<T, D>(a, (uint64_t)(blockIdx.x - work) * blockDim.x + threadIdx.x);
         return;
     }
-    const AppendBlock b = a.blocks[blockIdx.x / a.kv_heads];
-    const uint32_t head = blockIdx.x % a.kv_heads;
+    // (workgroups go to the 8 XCDs in turn: a block's heads to one of them, which has the rows of the table in its cache)
+    uint32_t block = blockIdx.x / a.kv_heads, head = blockIdx.x % a.kv_heads;
+    if (blockIdx.x < a.n_blocks / 8 * 8 * a.kv_heads) {
+        block = blockIdx.x / 8 / a.kv_heads * 8 + blockIdx.x % 8;
+        head = blockIdx.x / 8 % a.kv_heads;
+    }
+    const AppendBlock b = a.blocks[block];
     append_codes<T, D>(a, b, head, most_of_wave);
 }
 

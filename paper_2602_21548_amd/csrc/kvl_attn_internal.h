@@ -74,8 +74,7 @@ struct kvl_attn_plan_s {
     uint32_t class_first[kvl::kAttnClasses + 1] = {};   // items of each class
     uint32_t n_join = 0, most_join_rows = 0, most_pieces = 0, n_append_blocks = 0, most_append_rows = 0;
     uint64_t off_items = 0, off_join = 0, off_tables = 0, off_blocks = 0, off_tokens = 0;    // bytes into the device array
-    uint64_t div_mul = 0;                               // t / block_tokens == t * div_mul >> div_shift for t < 2^31
-    uint32_t div_shift = 0;
+    uint32_t div_mul = 0, div_shift = 0;                // t / block_tokens == 2 t * div_mul >> 32 + div_shift for t < 2^31
 
     // the join's wavefronts for each row, and its workgroups for each tile of rows and head
     uint32_t join_waves() const { return most_pieces > 8 ? 4 : 1; }

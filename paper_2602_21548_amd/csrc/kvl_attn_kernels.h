@@ -28,8 +28,7 @@ struct AttnArgs {
     float *lse;
     float *workspace;
     uint64_t q_stride, out_stride;      // elements
-    uint64_t div_mul;
-    uint32_t div_shift, block_tokens;
+    uint32_t div_mul, div_shift, block_tokens;
     uint32_t kv_heads, group;
     uint32_t window, sinks;             // window: 2^31 where there is none
     float c;                            // scale * log2(e)
@@ -88,7 +87,7 @@ struct KeyPlace {
 };
 __device__ __forceinline__ KeyPlace find_key(const AttnArgs &a, const AttnItem &it, uint32_t place) {
     const uint32_t v = min(place, it.end - 1), t = v < it.sinks ? v : v + it.gap;
-    const uint32_t b = (uint32_t)((t * a.div_mul) >> a.div_shift);
+    const uint32_t b = __umulhi(2 * t, a.div_mul) >> a.div_shift;
     return {(uint32_t)a.tables[it.table + b], t - b * a.block_tokens};
 }
 // What a block's codes are multiplied by.
@@ -237,7 +236,7 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
     const uint32_t half = wave % HALVES, stream = wave / HALVES, first_tile = half * RT;
     char *mine = lds + wave * kWaveBytes;
     float *key_c = reinterpret_cast<float *>(mine + KT * RB), *key_log = key_c + KT, *key_over = key_log + KT;
-    const uint64_t row_pitch = (uint64_t)a.kv_heads * RB;
+    const uint32_t row_pitch = a.kv_heads * RB;
     const char *k_head = a.k + head * RB, *v_head = a.v + head * RB;
 
     f32x4 o[RT][DC];
@@ -258,12 +257,12 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
         if (E4M3) scales = load_scales(a, at.block, head);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            const char *from = k_head + __shfl(rows, 16 * b + n) * row_pitch + g * 16;
+            const char *from = k_head + ((uint64_t)__shfl(rows, 16 * b + n) * row_pitch + g * 16);
 #pragma unroll
             for (int i = 0; i < KP; ++i) kn[b][i] = *reinterpret_cast<const u32x4 *>(from + 64 * i);
         }
 #pragma unroll
-        for (int i = 0; i < VP; ++i) vr[i] = *reinterpret_cast<const u32x4 *>(v_head + __shfl(rows, (i * 64 + lane) / PR) * row_pitch + lane % PR * 16);
+        for (int i = 0; i < VP; ++i) vr[i] = *reinterpret_cast<const u32x4 *>(v_head + ((uint64_t)__shfl(rows, (i * 64 + lane) / PR) * row_pitch + lane % PR * 16));
     };
 
     const uint32_t tiles = (it.end - it.begin + KT - 1) / KT;
@@ -531,7 +530,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
     const AttnItem it = a.items[blockIdx.x / a.kv_heads];
     const uint32_t head = blockIdx.x % a.kv_heads;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 32, h = lane / 32;
-    const uint64_t row_pitch = (uint64_t)a.kv_heads * PR * 16;
+    const uint32_t row_pitch = a.kv_heads * PR * 16;
     const char *k_head = a.k + head * PR * 16, *v_head = a.v + head * PR * 16;
     const uint32_t fetched = threadIdx.x / PR, piece = threadIdx.x % PR;
 
@@ -563,7 +562,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
         if (E4M3) scales = load_scales(a, at.block, head);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const uint64_t from = __shfl(rows, i * RP + fetched) * row_pitch + piece * 16;
+            const uint64_t from = (uint64_t)__shfl(rows, i * RP + fetched) * row_pitch + piece * 16;
             kr[i] = *reinterpret_cast<const u32x4 *>(k_head + from);
             vr[i] = *reinterpret_cast<const u32x4 *>(v_head + from);
         }

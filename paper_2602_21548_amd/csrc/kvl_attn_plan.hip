@@ -31,15 +31,19 @@ static Places places_of(const kvl_attn_layout_t &l, uint64_t first, uint64_t las
 //
 // A workgroup costs what `more` keys cost beside its own (finding its work, the first keys' way from memory, joining); the machine has room
 // for `slots` of them at once.  Up to that many run side by side, and the longest counts; more of them come in rounds, the last of
-// which is half empty on average; where anything is cut, the results have to be joined.  The length is the one, of a row of them, for which this
+// which is half empty on average; where anything is cut, the results have to be joined: written and read in 32 bits, `join` keys' time for each
+// workgroup at the rate at which all of them together take keys.  The length is the one, of a row of them, for which this
 // is least.  Whole steps are tiles for every wavefront.
 struct Machine {
     uint32_t step, more, slots;
+    double join;
 };
 constexpr uint32_t kJoinKeys = 256;
 static Machine machine_of(const kvl_attn_layout_t &l, uint32_t c) {
-    if (c == kRows128) return {kManyRowsTile, 256, 512};
-    return {(c == kRows64 ? 2 : 4) * few_rows_tile(l.head_dim), 512, l.cache_dtype == KVL_E4M3 && c == kRows16 ? 768u : 512u};
+    // (128 rows: 133 KB of results go by at 4.5 TB/s in 30 ns, a key of 512 workgroups takes 40.  Few rows: the bytes of a result's twice over those of a key)
+    if (c == kRows128) return {kManyRowsTile, 256, 512, 0.75};
+    const uint32_t slots = l.cache_dtype == KVL_E4M3 && c == kRows16 ? 768 : 512;
+    return {(c == kRows64 ? 2 : 4) * few_rows_tile(l.head_dim), 512, slots, 4.0 * kClassRows[c] / (element_bytes(l.cache_dtype) * slots)};
 }
 static uint64_t piece_of(const kvl_attn_layout_t &l, uint32_t c, const std::vector<Tile> &tiles) {
     const Machine m = machine_of(l, c);
@@ -57,15 +61,17 @@ static uint64_t piece_of(const kvl_attn_layout_t &l, uint32_t c, const std::vect
     // (with tiles enough for many rounds only those that are long beside the others are worth a cut)
     const uint64_t from = n_tiles * l.kv_heads > 8ull * m.slots ? std::max<uint64_t>(m.step, keys / n_tiles / m.step * m.step) : m.step;
     for (uint64_t piece = whole; piece >= from; piece = piece > m.step ? std::max<uint64_t>(m.step, piece * 7 / 8 / m.step * m.step) : 0) {
-        uint64_t count = 0, most = 0;
+        uint64_t count = 0, most = 0, cut = 0;
         for (const Tile &t : tiles) {
             if (t.cls != c) continue;
             const uint64_t n = t.at.end - t.at.begin, k = std::max<uint64_t>(1, (n + piece - 1) / piece);
             count += k;
+            if (k > 1) cut += k;
             most = std::max(most, (n + k - 1) / k);
         }
         const double rounds = (double)(count * l.kv_heads) / m.slots, mean = (double)keys / (double)count + m.more;
-        const double time = std::max((double)(most + m.more), rounds > 1 ? (rounds + 0.5) * mean : 0.0) + (count > n_tiles ? kJoinKeys : 0);
+        const double time = std::max((double)(most + m.more), rounds > 1 ? (rounds + 0.5) * mean : 0.0) +
+                            (cut ? kJoinKeys + m.join * (double)(cut * l.kv_heads) : 0.0);
         if (piece == whole || time < least) {
             least = time;
             best = piece;
@@ -118,8 +124,9 @@ static int build_attn(const kvl_attn_layout_t *layout, const kvl_request_t *req,
     plan->base.layout.row_bytes[0] = plan->base.layout.row_bytes[1] = l.kv_heads * l.head_dim * element_bytes(l.cache_dtype);
     plan->base.layout.pool_blocks = l.pool_blocks;
     while ((1ull << plan->div_shift) < bs) ++plan->div_shift;
-    plan->div_shift += 31;
-    plan->div_mul = (1ull << plan->div_shift) / bs + ((1ull << plan->div_shift) % bs != 0);
+    // ((2^(31 + shift) + bs - 1) / bs is at least 2^31, and below 2^32 as bs is above 2^(shift - 1))
+    plan->div_mul = (uint32_t)(((1ull << (31 + plan->div_shift)) + bs - 1) / bs);
+    if (plan->div_shift == 32) plan->div_mul = plan->div_shift = 0;     // (a block holds every token: 0)
 
     std::vector<uint64_t> token0(n_req), table0(n_req);
     uint64_t tokens = 0, entries = 0;
