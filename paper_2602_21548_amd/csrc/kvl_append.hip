@@ -322,9 +322,9 @@ __global__ void __launch_bounds__(256, 3) kvl_append_codes_kernel(const AppendAr
 }
 
 // Up to so many tasks the queries go in the launch of an 8-bit cache's keys and values, beyond in one of their own: its kernel wants a third of
-// the registers.  (32 heads of 128 beside 8, us in one / two: 256 tasks a token, 512 tokens 13.8 / 17.5, 4096 29.3 / 37.0, 8192 59.7 / 65.0, 16384 114 /
-// 109, 32768 227 / 205.)
-constexpr uint64_t kOneLaunchTasks = 3u << 20;
+// the registers.  (32 heads of 128 beside 8, 256 tasks a token, us in one / two: 64 tokens 7.5 / 10.4, 4096 24.0 / 29.5, 8192 47 / 56, 16384 90 / 93,
+// 32768 177 / 170.)
+constexpr uint64_t kOneLaunchTasks = 5u << 20;
 
 template <typename T, int D>
 static void launch_append(const kvl_attn_plan_t *plan, AppendArgs a, AttnLaunch &go) {

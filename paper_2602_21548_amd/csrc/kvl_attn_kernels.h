@@ -13,6 +13,8 @@
 // are taken in the order in which they lie there.  V^T is read in that order, by the transposing reads of the LDS.
 #pragma once
 
+#include <type_traits>
+
 #include "kvl_attn_internal.h"
 #include "kvl_attn_types.h"
 
@@ -233,7 +235,7 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
     const AttnItem it = a.items[item];
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 16, g = lane / 16;
     constexpr uint32_t kStreams = 4 / HALVES;
-    const uint32_t half = wave % HALVES, stream = wave / HALVES, first_tile = half * RT;
+    const uint32_t half = wave % HALVES, stream = wave / HALVES;     // (half: row tiles half, half + HALVES, ..)
     char *mine = lds + wave * kWaveBytes;
     float *key_c = reinterpret_cast<float *>(mine + KT * RB), *key_log = key_c + KT, *key_over = key_log + KT;
     const uint32_t row_pitch = a.kv_heads * RB;
@@ -265,7 +267,7 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
         for (int i = 0; i < VP; ++i) vr[i] = *reinterpret_cast<const u32x4 *>(v_head + ((uint64_t)__shfl(rows, (i * 64 + lane) / PR) * row_pitch + lane % PR * 16));
     };
 
-    const uint32_t tiles = (it.end - it.begin + KT - 1) / KT;
+    const uint32_t tiles = half * 16 < it.n_rows ? (it.end - it.begin + KT - 1) / KT : 0;
     KeyPlace next{};
     if (stream < tiles) {
         const KeyPlace first = find_key(a, it, it.begin + stream * KT + lane % KT);
@@ -322,16 +324,20 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
             fetch(next);
             if (tile + 2 * kStreams < tiles) next = find_key(a, it, it.begin + (tile + 2 * kStreams) * KT + lane % KT);
         }
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            if (HALVES > 1 && (first_tile + r) * 16 >= it.n_rows) continue;
+        // Row tiles one after the other, but both together over an 8-bit cache: keys and values become T once for them.
+        auto work = [&](auto first, auto count) {
+            constexpr int R0 = decltype(first)::value, R = decltype(count)::value;
             // scores: lane (n, g) gets row n's of keys 16 b + 4 g + i
-            f32x4 s[NB];
+            f32x4 s[R][NB];
 #pragma unroll
-            for (int b = 0; b < NB; ++b) s[b] = f32x4{0, 0, 0, 0};
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int b = 0; b < NB; ++b) s[r][b] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
-                const x8 x = kStaged ? staged[(first_tile + r) * CH + j][lane] : q[kStaged ? 0 : j];
+                x8 x[R];
+#pragma unroll
+                for (int r = 0; r < R; ++r) x[r] = kStaged ? staged[((R0 + r) * HALVES + half) * CH + j][lane] : q[kStaged ? 0 : j];
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
                     x8 k;
@@ -343,57 +349,59 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
                     } else {
                         k = __builtin_bit_cast(x8, kr[b][j]);
                     }
-                    s[b] = T::mma16(k, x, s[b]);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) s[r][b] = T::mma16(k, x[r], s[r][b]);
                 }
             }
-            float top = -__builtin_inff();
+            x8 p[R][NB / 2];
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                const int at_key = 16 * b + 4 * g;
-                const f32x4 kc = E4M3 ? *reinterpret_cast<const f32x4 *>(key_c + at_key) : f32x4{a.c, a.c, a.c, a.c};
-                const f32x4 kl = E4M3 ? *reinterpret_cast<const f32x4 *>(key_log + at_key) : f32x4{0, 0, 0, 0};
+            for (int r = 0; r < R; ++r) {
+                float top = -__builtin_inff();
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    s[b][i] = E4M3 ? __builtin_fmaf(s[b][i], kc[i], kl[i]) : s[b][i] * kc[i];
+                for (int b = 0; b < NB; ++b) {
+                    const int at_key = 16 * b + 4 * g;
+                    const f32x4 kc = E4M3 ? *reinterpret_cast<const f32x4 *>(key_c + at_key) : f32x4{a.c, a.c, a.c, a.c};
+                    const f32x4 kl = E4M3 ? *reinterpret_cast<const f32x4 *>(key_log + at_key) : f32x4{0, 0, 0, 0};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[r][b][i] = E4M3 ? __builtin_fmaf(s[r][b][i], kc[i], kl[i]) : s[r][b][i] * kc[i];
                 }
-            }
-            if (!whole) {
-                const Seen seen = kStaged ? seen_of[(first_tile + r) * 16 + n] : seen_here;
+                if (!whole) {
+                    const Seen seen = kStaged ? seen_of[((R0 + r) * HALVES + half) * 16 + n] : seen_here;
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (!seen(v0 + 16 * b + 4 * g + i)) s[r][b][i] = -__builtin_inff();
+                }
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (!seen(v0 + 16 * b + 4 * g + i)) s[b][i] = -__builtin_inff();
-            }
+                    for (int i = 0; i < 4; ++i) top = fmaxf(top, s[r][b][i]);
+                top = max_quarters(top);
+                if (__any(top > m[R0 + r] + kSlack)) {
+                    const float to = fmaxf(m[R0 + r], top), f = factor(m[R0 + r], to);
+                    m[R0 + r] = to;
+                    l[R0 + r] *= f;
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[b][i]);
-            top = max_quarters(top);
-            if (__any(top > m[r] + kSlack)) {
-                const float to = fmaxf(m[r], top), f = factor(m[r], to);
-                m[r] = to;
-                l[r] *= f;
-#pragma unroll
-                for (int d = 0; d < DC; ++d) o[r][d] *= f;
-            }
-            const float from = m[r] == -__builtin_inff() ? 0.f : m[r] - kLift<T>;
-            x8 p[NB / 2];
-#pragma unroll
-            for (int b = 0; b < NB; b += 2) {
-                u32x4 w;
-#pragma unroll
-                for (int bb = b; bb < b + 2; ++bb) {
-                    const f32x4 over = E4M3 ? *reinterpret_cast<const f32x4 *>(key_over + 16 * bb + 4 * g) : f32x4{1, 1, 1, 1};
-#pragma unroll
-                    for (int i = 0; i < 4; i += 2) {
-                        const float x = __builtin_amdgcn_exp2f(s[bb][i] - from), y = __builtin_amdgcn_exp2f(s[bb][i + 1] - from);
-                        if (E4M3) l[r] = __builtin_fmaf(y, over[i + 1], __builtin_fmaf(x, over[i], l[r]));
-                        else l[r] += x + y;
-                        w[bb % 2 * 2 + i / 2] = narrow<T>(x, y);
-                    }
+                    for (int d = 0; d < DC; ++d) o[R0 + r][d] *= f;
                 }
-                p[b / 2] = __builtin_bit_cast(x8, w);
+                const float from = m[R0 + r] == -__builtin_inff() ? 0.f : m[R0 + r] - kLift<T>;
+#pragma unroll
+                for (int b = 0; b < NB; b += 2) {
+                    u32x4 w;
+#pragma unroll
+                    for (int bb = b; bb < b + 2; ++bb) {
+                        const f32x4 over = E4M3 ? *reinterpret_cast<const f32x4 *>(key_over + 16 * bb + 4 * g) : f32x4{1, 1, 1, 1};
+#pragma unroll
+                        for (int i = 0; i < 4; i += 2) {
+                            const float x = __builtin_amdgcn_exp2f(s[r][bb][i] - from), y = __builtin_amdgcn_exp2f(s[r][bb][i + 1] - from);
+                            if (E4M3) l[R0 + r] = __builtin_fmaf(y, over[i + 1], __builtin_fmaf(x, over[i], l[R0 + r]));
+                            else l[R0 + r] += x + y;
+                            w[bb % 2 * 2 + i / 2] = narrow<T>(x, y);
+                        }
+                    }
+                    p[r][b / 2] = __builtin_bit_cast(x8, w);
+                }
             }
             // outputs: lane (n, g) gets row n's elements 16 d + 4 g + i; the contraction's keys of lane group g are 4 g .. + 3 and 16 + 4 g .. + 3
 #pragma unroll
@@ -412,9 +420,19 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
                         const u32x2 y = read_columns16(mine + (row + 16) * RB + ((d ^ ((row + 16) & kSwizzle)) << 5) + (n & 3) * 8);
                         w = u32x4{x[0], x[1], y[0], y[1]};
                     }
-                    o[r][d] = T::mma16(__builtin_bit_cast(x8, w), p[u], o[r][d]);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) o[R0 + r][d] = T::mma16(__builtin_bit_cast(x8, w), p[r][u], o[R0 + r][d]);
                 }
-                    }
+        };
+        typedef std::integral_constant<int, 0> Zero;
+        typedef std::integral_constant<int, 1> One;
+        const bool second = RT > 1 && (HALVES + half) * 16 < it.n_rows;
+        if (E4M3 && second) {
+            work(Zero{}, std::integral_constant<int, RT>{});
+        } else {
+            work(Zero{}, One{});
+            if (!E4M3 && second) work(std::integral_constant<int, RT - 1>{}, One{});
+        }
         if (odd) {
             for (uint32_t j = 0; j < KT && v0 + j < it.end; ++j) {
                 const uint32_t row = __shfl(now_rows, (int)j);
@@ -423,7 +441,7 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
                     const f32x4 e = odd_values<T, E4M3, D>(a, head, row, 16 * d + 4 * g);
 #pragma unroll
                     for (int r = 0; r < RT; ++r)
-                        if ((kStaged ? seen_of[(first_tile + r) * 16 + n] : seen_here)(v0 + j)) o[r][d] += e;
+                        if ((kStaged ? seen_of[(r * HALVES + half) * 16 + n] : seen_here)(v0 + j)) o[r][d] += e;
                 }
             }
         }
@@ -452,7 +470,7 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
         __syncthreads();
 #pragma unroll
         for (uint32_t hh = 0; hh < HALVES; ++hh) {
-            const uint32_t i = (hh * RT + r) * 16 + row;
+            const uint32_t i = (r * HALVES + hh) * 16 + row;
             if (i >= it.n_rows) continue;
             float most = -__builtin_inff(), sum = 0, e[E] = {};
             for (uint32_t w = hh; w < 4; w += HALVES) most = fmaxf(most, state[w][r * 16 + row][0]);
