@@ -585,6 +585,9 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
             vr[i] = *reinterpret_cast<const u32x4 *>(v_head + from);
         }
     };
+    // Where a lane reads the first of its 16 bytes of K, and of its 8 of V, of a tile: the others are there with bits turned.
+    uint32_t k_at = n * RB + ((h ^ k_turn(n)) << 4);
+    uint32_t v_at = (4 * h + lane % 16 / 4) * RB + (((2 * (lane / 16 % 2) + lane % 4 / 2) ^ v_turn(lane % 16 / 4)) << 4) + lane % 2 * 8;
     if (threadIdx.x < 3) odd_tile[threadIdx.x] = 0;
     __syncthreads();
     const uint32_t tiles = (it.end - it.begin + KT - 1) / KT;
@@ -619,7 +622,6 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
                 *reinterpret_cast<u32x4 *>(v_lds + r * RB + ((piece ^ v_turn(r)) << 4)) = vr[i];
             }
         }
-        const uint32_t now_rows = rows;
         if (tile + 1 < tiles) {
             fetch(next);
             if (tile + 2 < tiles) next = find_key(a, it, v0 + 2 * KT + lane);
@@ -628,6 +630,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
         const bool odd = odd_tile[tile % 3] != 0;
         if (threadIdx.x == 0) odd_tile[(tile + 2) % 3] = 0;
 
+        asm volatile("" : "+v"(k_at), "+v"(v_at));      // (the addresses made of them are made anew for each tile: registers are short)
         // a tile that none of the wavefront's rows sees
         const uint32_t v1 = min(v0 + KT, it.end) - 1;
         const uint32_t t0 = v0 < it.sinks ? v0 : v0 + it.gap, t1 = v1 < it.sinks ? v1 : v1 + it.gap;
@@ -642,7 +645,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
             for (int i = 0; i < 16; ++i) s[b][i] = 0;
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
-                const x8 k = *reinterpret_cast<const x8 *>(k_lds + (32 * b + n) * RB + (((2 * j + h) ^ k_turn(n)) << 4));
+                const x8 k = *reinterpret_cast<const x8 *>(k_lds + 32 * b * RB + (k_at ^ j << 5));
                 s[b] = T::mma32(k, q[j], s[b]);
             }
         }
@@ -688,14 +691,14 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
         for (int u = 0; u < 4; ++u)
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
-                const uint32_t r = 16 * u + 4 * h + lane % 16 / 4, at = 4 * d + 2 * (lane / 16 % 2) + lane % 4 / 2;
-                const u32x2 x = read_columns16(v_lds + r * RB + ((at ^ v_turn(r)) << 4) + lane % 2 * 8);
-                const u32x2 y = read_columns16(v_lds + (r + 8) * RB + ((at ^ v_turn(r + 8)) << 4) + lane % 2 * 8);
+                const char *at = v_lds + 16 * u * RB + (v_at ^ d << 6);
+                const u32x2 x = read_columns16(at), y = read_columns16(at + 8 * RB);
                 o[d] = T::mma32(__builtin_bit_cast(x8, (u32x4{x[0], x[1], y[0], y[1]})), p[u], o[d]);
             }
         if (odd) {
             for (uint32_t j = 0; j < KT && v0 + j < it.end; ++j) {
-                const uint32_t pool_row = __shfl(now_rows, (int)j);
+                const KeyPlace place = find_key(a, it, v0 + j);
+                const uint32_t pool_row = place.block * a.block_tokens + place.row_in_block;
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
 #pragma unroll
