@@ -3,7 +3,8 @@
 // Pairs (a, b) of a head's leading rope_dim elements become (a cos - b sin, b cos + a sin).  A lane takes two pieces of 8 elements of a
 // head: those at j and j + rope_dim/2, whose elements are pairs (halves), else two that are half of what there is apart, so that neighbouring
 // lanes' pieces are neighbours in memory in each load and store.  The cosines and sines are a row of the table, which the heads of a token
-// share in the caches.  Memory bounds both kernels: each element is read once and written once.
+// share in the caches.  Memory bounds both kernels: each element is read once and written once.  9131 tokens of 16 + 2 * 4 heads of 128, 16-bit cache:
+// 115 MB in 23.2 us, 4.9 TB/s, the rate of a large copy; 40800 of 32 + 2 * 8, 8-bit cache: 940 MB in 196 us, 4.8 TB/s, of which the queries take 110.
 #include "kvl_attn_internal.h"
 #include "kvl_attn_types.h"
 
@@ -239,17 +240,24 @@ __device__ __forceinline__ void append_codes(const AppendArgs &a, const AppendBl
         *reinterpret_cast<u32x2 *>(to + at.second) = u32x2{codes4(e + 8, scale, over, odd), codes4(e + 12, scale, over, odd)};
     };
 
-    float e[2][N][16], most[2] = {0, 0};
+    // (values wait as they came: in half the registers)
+    float e[N][16], most[2] = {0, 0};
+    u32x4 raw[N][2];
     bool odd[2][N] = {};
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const uint32_t i = threadIdx.x + j * per;
-            if (i >= n) continue;
-            load(planes[x], i, e[x][j]);
-            most[x] = largest(e[x][j], most[x], &odd[x][j]);
-        }
+    for (int j = 0; j < N; ++j) {
+        const uint32_t i = threadIdx.x + j * per;
+        if (i >= n) continue;
+        const Pieces at = pieces_of<D>(i % kHeadTasks, a.rope_dim, a.rope_pairs, false);
+        const char *x = planes[1].from + i / kHeadTasks * planes[1].stride;
+        raw[j][0] = *reinterpret_cast<const u32x4 *>(x + 2 * at.first);
+        raw[j][1] = *reinterpret_cast<const u32x4 *>(x + 2 * at.second);
+        load(planes[0], i, e[j]);
+        most[0] = largest(e[j], most[0], &odd[0][j]);
+        float w[16];
+        widen16<T>(raw[j][0], raw[j][1], w);
+        most[1] = largest(w, most[1], &odd[1][j]);
+    }
     for (uint32_t i = threadIdx.x + N * per; i < n; i += per)
         for (int x = 0; x < 2; ++x) {
             float w[16];
@@ -291,7 +299,14 @@ __device__ __forceinline__ void append_codes(const AppendArgs &a, const AppendBl
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const uint32_t i = threadIdx.x + j * per;
-            if (i < n) store(plane, i, e[x][j], scale, over, odd[x][j]);
+            if (i >= n) continue;
+            if (x == 0) {
+                store(plane, i, e[j], scale, over, odd[0][j]);
+            } else {
+                float w[16];
+                widen16<T>(raw[j][0], raw[j][1], w);
+                store(plane, i, w, scale, over, odd[1][j]);
+            }
         }
         for (uint32_t i = threadIdx.x + N * per; i < n; i += per) {
             float w[16];
@@ -303,6 +318,7 @@ __device__ __forceinline__ void append_codes(const AppendArgs &a, const AppendBl
 }
 
 // 8-bit caches: a workgroup for each block that receives rows and each head, and after those workgroups for the queries.
+// (Three wavefronts a SIMD, and nothing in scratch memory, which costs every workgroup its start: two 235 us, three with 24 bytes of scratch 211, so 196.)
 template <typename T, int D>
 __global__ void __launch_bounds__(256, 3) kvl_append_codes_kernel(const AppendArgs a) {
     __shared__ f32x2 most_of_wave[4];
@@ -322,8 +338,8 @@ __global__ void __launch_bounds__(256, 3) kvl_append_codes_kernel(const AppendAr
 }
 
 // Up to so many tasks the queries go in the launch of an 8-bit cache's keys and values, beyond in one of their own: its kernel wants a third of
-// the registers.  (32 heads of 128 beside 8, 256 tasks a token, us in one / two: 64 tokens 7.5 / 10.4, 4096 24.0 / 29.5, 8192 47 / 56, 16384 90 / 93,
-// 32768 177 / 170.)
+// the registers.  (32 heads of 128 beside 8, 256 tasks a token, us in one / two: 64 tokens 7.0 / 10.9, 4096 22.9 / 28.6, 8192 46 / 53, 16384 86 / 89,
+// 32768 168 / 160.)
 constexpr uint64_t kOneLaunchTasks = 5u << 20;
 
 template <typename T, int D>

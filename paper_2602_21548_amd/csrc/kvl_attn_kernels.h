@@ -204,7 +204,8 @@ __device__ __forceinline__ void write_lse(const AttnArgs &a, uint32_t token0, ui
 // to the registers of the matrix instructions as it lies: lane (n, g) has key n's elements of four-lane group g, and the queries are laid out
 // to match.  V goes through the wavefront's own part of the LDS, which turns it.  8-bit codes become T there and here, exactly; their
 // scales multiply scores (K) and join the exponent (V: with x = c s_k <q, K_t> + log2 s_v, 2^(x - m) multiplies the codes, and 2^(x - m) / s_v
-// is the term of l), in 32 bits, whatever T is.
+// is the term of l), in 32 bits, whatever T is.  A step of 64 requests of 16-64 K tokens, 64 + 8 heads, 8 bits: 5.3 GB at 5.6 TB/s; of 128 under a window
+// of 4096, 16 bits: 2.0 GB at 5.6 TB/s.
 //
 // Beyond 32 rows the registers do not hold a wavefront's outputs beside what is on its way, and scratch memory's loads come in order behind those of
 // the next keys: there HALVES = 2, and two wavefronts take the same tile of keys, half of the rows each; what the second one loads is in the caches.
@@ -496,10 +497,13 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
 
 // Many rows ------------------------------------------------------------------------------------------------------------------------
 //
-// 128 rows, 32 for each wavefront, against pieces of their keys in tiles of 64 that the wavefronts share in the LDS.  The matrix
-// instructions bound it, with the exponentials and the LDS's reads close behind.  A tile comes by way of registers, while the tile before is
-// worked on; 8-bit codes become T there, once for all rows, with their scales: exactly where these are powers of two, else with one more
-// rounding to T.
+// 128 rows, 32 for each wavefront, against pieces of their keys in tiles of 64 that the wavefronts share in the LDS.  A tile comes by way of
+// registers, while the tile before is worked on; 8-bit codes become T there, once for all rows, with their scales: exactly where these are powers
+// of two, else with one more rounding to T.
+//
+// The matrix instructions (37 % of the time busy) and the vector unit (46 %, most of it the exponentials and what goes with them) bound it, which
+// the two wavefronts that a SIMD has registers for do not overlap well: 850 TFLOP/s in 8-bit tails over long prefixes, heads of 128; of 64, 26 % and
+// 54 %, 630 under a window.
 template <typename T, bool E4M3>
 __device__ __forceinline__ void codes_to_half(u32x4 w, float scale, u32x4 *x, u32x4 *y) {
     uint32_t e[8];
