@@ -178,6 +178,16 @@ __device__ __forceinline__ f32x4 odd_values(const AttnArgs &a, uint32_t head, ui
 // 2^(m - to), where neither may be there yet (-inf)
 __device__ __forceinline__ float factor(float m, float to) { return m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - to); }
 
+// Two floats as bf16 numbers, and what these leave.
+struct TwoParts {
+    uint32_t first, rest;
+};
+__device__ __forceinline__ TwoParts two_parts(float x, float y) {
+    const uint32_t first = narrow<Bf16>(x, y);
+    const f32x2 there = Bf16::widen(first);
+    return {first, narrow<Bf16>(x - there[0], y - there[1])};
+}
+
 // The output of one row: its sum, maximum and E unnormalised elements from `dim` on.
 template <typename T, int E>
 __device__ __forceinline__ void write_row(const AttnArgs &a, uint32_t token0, uint32_t row, uint32_t head, uint32_t dim, int head_dim, float l, const float (&o)[E]) {
@@ -499,7 +509,9 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
 //
 // 128 rows, 32 for each wavefront, against pieces of their keys in tiles of 64 that the wavefronts share in the LDS.  A tile comes by way of
 // registers, while the tile before is worked on; 8-bit codes become T there, once for all rows, with their scales: exactly where these are powers
-// of two, else with one more rounding to T.
+// of two, else with one more rounding to T.  fp16 holds every code times 2^-15 to 2^7 and not much more: a tile with a scale outside of that has
+// its codes alone there, keys' as fp16, values' as bf16; the keys' scales multiply scores, the values' the weights, in 32 bits, and a weight is two
+// bf16 numbers, the second one what the first leaves (their products with codes are exact, and a weight keeps 16 bits).
 //
 // The matrix instructions (37 % of the time busy) and the vector unit (46 %, most of it the exponentials and what goes with them) bound it, which
 // the two wavefronts that a SIMD has registers for do not overlap well: 850 TFLOP/s in 8-bit tails over long prefixes, heads of 128; of 64, 26 % and
@@ -521,16 +533,12 @@ __device__ __forceinline__ void codes_to_half(u32x4 w, float scale, u32x4 *x, u3
             e[i] = narrow<T>(v[0] * rest, v[1] * rest);
         }
     }
-    if (T::kExponent == F16::kExponent && __any(scale >= 128.f)) {         // beyond fp16's range: its largest
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if ((e[i] & 0x7fffu) == 0x7c00u) e[i] -= 1;
-            if ((e[i] & 0x7fff0000u) == 0x7c000000u) e[i] -= 0x10000u;
-        }
-    }
     *x = u32x4{e[0], e[1], e[2], e[3]};
     *y = u32x4{e[4], e[5], e[6], e[7]};
 }
+
+// Scales that leave codes in fp16's range.
+__device__ __forceinline__ bool suits_f16(float scale) { return scale >= 0x1p-15f && scale <= 0x1p7f; }
 
 template <typename T, bool E4M3, int D>
 __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(const AttnArgs a) {
@@ -541,6 +549,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
     constexpr int N = KT / RP;                                      // a lane's pieces of a tile
     constexpr int CH = D / 16, DB = D / 32;                         // steps of the first product; blocks of the output
     static_assert(KT % RP == 0 && KT == 64, "whole pieces; a key a lane");
+    constexpr bool kNarrow = E4M3 && T::kExponent == F16::kExponent;    // some scales do not go into T
     // Pieces of 16 bytes are turned by their row's number so that the 16 rows that lanes read of K together, and the 4 rows by 64 bytes of V, lie in
     // different banks (256 bytes of them): rows of 128 bytes take half of these each.
     auto k_turn = [](uint32_t r) { return D == 128 ? r & 15 : r >> 1 & 7; };
@@ -610,21 +619,35 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
             make_plain<T, E4M3>(vr);
         }
         const Scales by{in_range(scales.k), in_range(scales.v)};
+        // (the same in all wavefronts: each has every key's scales)
+        const bool apart = kNarrow && __builtin_amdgcn_readfirstlane(__any(!suits_f16(by.k) || !suits_f16(by.v)));
+        // (one branch around all of it: 32-K tails in fp16 784 us, one at each value 812, without the second form 768)
+        auto convert = [&](auto key_type, auto value_type, Scales times) {
+            typedef decltype(key_type) TK;
+            typedef decltype(value_type) TV;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const uint32_t r = i * RP + fetched;
-            if (E4M3) {
+            for (int i = 0; i < N; ++i) {
+                const uint32_t r = i * RP + fetched;
                 u32x4 x, y;
-                codes_to_half<T, E4M3>(kr[i], __shfl(by.k, (int)r), &x, &y);
+                codes_to_half<TK, E4M3>(kr[i], __shfl(times.k, (int)r), &x, &y);
                 *reinterpret_cast<u32x4 *>(k_lds + r * RB + (((2 * piece) ^ k_turn(r)) << 4)) = x;
                 *reinterpret_cast<u32x4 *>(k_lds + r * RB + (((2 * piece + 1) ^ k_turn(r)) << 4)) = y;
-                codes_to_half<T, E4M3>(vr[i], __shfl(by.v, (int)r), &x, &y);
+                codes_to_half<TV, E4M3>(vr[i], __shfl(times.v, (int)r), &x, &y);
                 *reinterpret_cast<u32x4 *>(v_lds + r * RB + (((2 * piece) ^ v_turn(r)) << 4)) = x;
                 *reinterpret_cast<u32x4 *>(v_lds + r * RB + (((2 * piece + 1) ^ v_turn(r)) << 4)) = y;
-            } else {
+            }
+        };
+        if (!E4M3) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const uint32_t r = i * RP + fetched;
                 *reinterpret_cast<u32x4 *>(k_lds + r * RB + ((piece ^ k_turn(r)) << 4)) = kr[i];
                 *reinterpret_cast<u32x4 *>(v_lds + r * RB + ((piece ^ v_turn(r)) << 4)) = vr[i];
             }
+        } else if (apart) {
+            convert(T{}, Bf16{}, Scales{1.f, 1.f});
+        } else {
+            convert(T{}, T{}, by);
         }
         if (tile + 1 < tiles) {
             fetch(next);
@@ -653,6 +676,18 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
                 s[b] = T::mma32(k, q[j], s[b]);
             }
         }
+        // what the lane of key `key` + 4 h has (its address made anew each time, too)
+        auto of_key = [&](float x, int key) {
+            int at = (int)(16 * h);
+            asm volatile("" : "+v"(at));
+            return __uint_as_float((uint32_t)__builtin_amdgcn_ds_bpermute(at + 4 * key, (int)__float_as_uint(x)));
+        };
+        if (apart) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[b][i] *= of_key(by.k, 32 * b + 8 * (i / 4) + i % 4);
+        }
         if (!whole) {
 #pragma unroll
             for (int b = 0; b < 2; ++b)
@@ -677,28 +712,60 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
                 for (int i = 0; i < 16; ++i) o[d][i] *= f;
         }
         const float from = m == -__builtin_inff() ? 0.f : kLift<T> - m;
-        x8 p[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            u32x4 w;
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u / 2][8 * (u % 2) + i], a.c, from));
-                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u / 2][8 * (u % 2) + i + 1], a.c, from));
-                l += x + y;
-                w[i / 2] = narrow<T>(x, y);
-            }
-            p[u] = __builtin_bit_cast(x8, w);
-        }
+        // the weights of keys 16 u + 8 (i / 4) + 4 h + i % 4 and the next, i even
+        auto weights = [&](int u, int i) {
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u / 2][8 * (u % 2) + i], a.c, from));
+            const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u / 2][8 * (u % 2) + i + 1], a.c, from));
+            l += x + y;
+            return f32x2{x, y};
+        };
+        auto values = [&](int u, int d) {
+            const char *at = v_lds + 16 * u * RB + (v_at ^ d << 6);
+            const u32x2 x = read_columns16(at), y = read_columns16(at + 8 * RB);
+            return u32x4{x[0], x[1], y[0], y[1]};
+        };
         // outputs: lane (n, h) gets row n's elements 32 d + 8 (i / 4) + 4 h + i % 4
+        if (apart) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+            for (int u = 0; u < 4; ++u) {
+                u32x4 first, rest;
 #pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                const char *at = v_lds + 16 * u * RB + (v_at ^ d << 6);
-                const u32x2 x = read_columns16(at), y = read_columns16(at + 8 * RB);
-                o[d] = T::mma32(__builtin_bit_cast(x8, (u32x4{x[0], x[1], y[0], y[1]})), p[u], o[d]);
+                for (int i = 0; i < 8; i += 2) {
+                    const int key = 16 * u + 8 * (i / 4) + i % 4;
+                    const f32x2 x = weights(u, i);
+                    const TwoParts w = two_parts(x[0] * of_key(by.v, key), x[1] * of_key(by.v, key + 1));
+                    first[i / 2] = w.first;
+                    rest[i / 2] = w.rest;
+                }
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    const Bf16::x8 v = __builtin_bit_cast(Bf16::x8, values(u, d));
+                    o[d] = Bf16::mma32(v, __builtin_bit_cast(Bf16::x8, first), o[d]);
+                    o[d] = Bf16::mma32(v, __builtin_bit_cast(Bf16::x8, rest), o[d]);
+                }
             }
+        }
+        if (kNarrow) {          // (a branch after the other: outputs of one stay where they are for the other)
+#pragma unroll
+            for (int d = 0; d < DB; ++d) asm volatile("" : "+v"(o[d]));
+        }
+        if (!apart) {
+            x8 p[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                u32x4 w;
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) {
+                    const f32x2 x = weights(u, i);
+                    w[i / 2] = narrow<T>(x[0], x[1]);
+                }
+                p[u] = __builtin_bit_cast(x8, w);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int d = 0; d < DB; ++d) o[d] = T::mma32(__builtin_bit_cast(x8, values(u, d)), p[u], o[d]);
+        }
         if (odd) {
             for (uint32_t j = 0; j < KT && v0 + j < it.end; ++j) {
                 const KeyPlace place = find_key(a, it, v0 + j);
