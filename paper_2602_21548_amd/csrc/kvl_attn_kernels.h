@@ -214,8 +214,10 @@ __device__ __forceinline__ void write_lse(const AttnArgs &a, uint32_t token0, ui
 // to the registers of the matrix instructions as it lies: lane (n, g) has key n's elements of four-lane group g, and the queries are laid out
 // to match.  V goes through the wavefront's own part of the LDS, which turns it.  8-bit codes become T there and here, exactly; their
 // scales multiply scores (K) and join the exponent (V: with x = c s_k <q, K_t> + log2 s_v, 2^(x - m) multiplies the codes, and 2^(x - m) / s_v
-// is the term of l), in 32 bits, whatever T is.  A step of 64 requests of 16-64 K tokens, 64 + 8 heads, 8 bits: 5.3 GB at 5.6 TB/s; of 128 under a window
-// of 4096, 16 bits: 2.0 GB at 5.6 TB/s.
+// is the term of l), in 32 bits, whatever T is.  These weights span as much as the values' scales do, which is more than fp16 holds: for fp16 queries
+// values are bf16 there, exactly, and a weight is two bf16 numbers, as in the kernel for many rows (one token a request: no slower; 32 requests of 21 to 42 rows, heads
+// of 128: 49 us, with weights in fp16 45).  A step of 64 requests of 16-64 K tokens, 64 + 8 heads, 8 bits: 5.3 GB at 5.6 TB/s; of 128 under a
+// window of 4096, 16 bits: 2.0 GB at 5.6 TB/s.
 //
 // Beyond 32 rows the registers do not hold a wavefront's outputs beside what is on its way, and scratch memory's loads come in order behind those of
 // the next keys: there HALVES = 2, and two wavefronts take the same tile of keys, half of the rows each; what the second one loads is in the caches.
@@ -235,6 +237,10 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
     __shared__ __attribute__((aligned(16))) char lds[kBytes];
     __shared__ f32x2 state[4][RT * 16];
     typedef typename T::x8 x8;
+    // what values and weights are multiplied in
+    constexpr bool kTwoParts = E4M3 && T::kExponent == F16::kExponent;
+    typedef std::conditional_t<kTwoParts, Bf16, T> TV;
+    typedef typename TV::x8 TV8;
     // where there are several tiles of rows: queries, in the order in which the matrix instructions take them, and what each row sees
     constexpr bool kStaged = RT > 1;
     constexpr int kTiles = RT * HALVES;
@@ -364,7 +370,7 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
                     for (int r = 0; r < R; ++r) s[r][b] = T::mma16(k, x[r], s[r][b]);
                 }
             }
-            x8 p[R][NB / 2];
+            TV8 p[R][NB / 2], p_rest[R][NB / 2];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 float top = -__builtin_inff();
@@ -399,7 +405,7 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
                 const float from = m[R0 + r] == -__builtin_inff() ? 0.f : m[R0 + r] - kLift<T>;
 #pragma unroll
                 for (int b = 0; b < NB; b += 2) {
-                    u32x4 w;
+                    u32x4 w, rest;
 #pragma unroll
                     for (int bb = b; bb < b + 2; ++bb) {
                         const f32x4 over = E4M3 ? *reinterpret_cast<const f32x4 *>(key_over + 16 * bb + 4 * g) : f32x4{1, 1, 1, 1};
@@ -408,10 +414,17 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
                             const float x = __builtin_amdgcn_exp2f(s[r][bb][i] - from), y = __builtin_amdgcn_exp2f(s[r][bb][i + 1] - from);
                             if (E4M3) l[R0 + r] = __builtin_fmaf(y, over[i + 1], __builtin_fmaf(x, over[i], l[R0 + r]));
                             else l[R0 + r] += x + y;
-                            w[bb % 2 * 2 + i / 2] = narrow<T>(x, y);
+                            if (kTwoParts) {
+                                const TwoParts parts = two_parts(x, y);
+                                w[bb % 2 * 2 + i / 2] = parts.first;
+                                rest[bb % 2 * 2 + i / 2] = parts.rest;
+                            } else {
+                                w[bb % 2 * 2 + i / 2] = narrow<T>(x, y);
+                            }
                         }
                     }
-                    p[r][b / 2] = __builtin_bit_cast(x8, w);
+                    p[r][b / 2] = __builtin_bit_cast(TV8, w);
+                    if (kTwoParts) p_rest[r][b / 2] = __builtin_bit_cast(TV8, rest);
                 }
             }
             // outputs: lane (n, g) gets row n's elements 16 d + 4 g + i; the contraction's keys of lane group g are 4 g .. + 3 and 16 + 4 g .. + 3
@@ -423,8 +436,8 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
                     if (E4M3) {
                         const uint32_t j = n / 2, row = 32 * u + 4 * g + (j < 4 ? j : j + 12);
                         const u32x2 c = read_columns8(mine + row * RB + ((d ^ (row & kSwizzle)) << 4) + (n & 1) * 8);
-                        w = u32x4{T::template from_codes<false>(c[0], 1.f), T::template from_codes<true>(c[0], 1.f), T::template from_codes<false>(c[1], 1.f),
-                                  T::template from_codes<true>(c[1], 1.f)};
+                        w = u32x4{TV::template from_codes<false>(c[0], 1.f), TV::template from_codes<true>(c[0], 1.f), TV::template from_codes<false>(c[1], 1.f),
+                                  TV::template from_codes<true>(c[1], 1.f)};
                     } else {
                         const uint32_t row = 32 * u + 4 * g + n / 4;
                         const u32x2 x = read_columns16(mine + row * RB + ((d ^ (row & kSwizzle)) << 5) + (n & 3) * 8);
@@ -432,7 +445,10 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
                         w = u32x4{x[0], x[1], y[0], y[1]};
                     }
 #pragma unroll
-                    for (int r = 0; r < R; ++r) o[R0 + r][d] = T::mma16(__builtin_bit_cast(x8, w), p[r][u], o[R0 + r][d]);
+                    for (int r = 0; r < R; ++r) {
+                        o[R0 + r][d] = TV::mma16(__builtin_bit_cast(TV8, w), p[r][u], o[R0 + r][d]);
+                        if (kTwoParts) o[R0 + r][d] = TV::mma16(__builtin_bit_cast(TV8, w), p_rest[r][u], o[R0 + r][d]);
+                    }
                 }
         };
         typedef std::integral_constant<int, 0> Zero;

@@ -83,10 +83,30 @@ def test_many_rows_with_a_window_and_spoilt_values(dim):
     close(b, torch.from_numpy(np.where(keep, got, w_out)), lse, (w_out, w_lse, weight, reach))
 
 
+# a tile of 16 rows, two of them, and two wavefronts' two
+FEW = [([100, 0, 700], [1, 1, 1], (8, 2)), ([100, 410], [6, 5], (8, 2)), ([900], [12], (8, 2)), ([2600], [2], (8, 1))]
+
+
+@pytest.mark.parametrize("k_range,v_range", RANGES + [((-30, 20), (-20, 12))])
+@pytest.mark.parametrize("hit,app,heads", FEW)
+@pytest.mark.parametrize("dim,powers", [(64, True), (128, True), (128, False)])
+def test_few_rows(hit, app, heads, dim, k_range, v_range, powers):
+    b = scaled(hit, app, heads, dim, k_range, v_range, powers)
+    out, lse = attend(b)
+    torch.cuda.synchronize()
+    close(b, out, lse, wanted(b))
+
+
 # The first blocks' values are zeros under a scale 2^34 times that of the others: what the others hold is all there is.
 @pytest.mark.parametrize("app,heads", [(40, (8, 2)), (70, (2, 2))])
 @pytest.mark.parametrize("dim", [64, 128])
 def test_zeros_under_a_large_scale_many_rows(app, heads, dim):
+    zeros_under_a_large_scale(app, heads, dim)
+
+
+@pytest.mark.parametrize("app,heads", [(1, (8, 2)), (6, (8, 2)), (12, (8, 2))])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_zeros_under_a_large_scale_few_rows(app, heads, dim):
     zeros_under_a_large_scale(app, heads, dim)
 
 
