@@ -101,8 +101,8 @@ int kvl_attn_plan_items(const kvl_attn_plan_t *plan, kvl_attn_item_t *out, uint6
  *
  * 8-bit cache: the scale of a block and head is the power of two 2^e with the least e in [-32, 63]
  * for which no finite new value of the block is above 448 * 2^e; in a block that already holds hit
- * tokens it is at least the scale that is there, and where it grows the codes that are there are
- * rounded again to the new one.  (e4m3 floats: a power of two costs no precision, and the second rounding
+ * tokens it is at least the scale that is there (taken as kvl_attn_layer takes it, from 2^-32 to 2^63, NaN as
+ * 2^-32), and where it grows the codes that are there are rounded again to the new one.  (e4m3 floats: a power of two costs no precision, and the second rounding
  * loses only what falls below the least normal.)  Codes are rounded to the nearest, ties to even; what
  * is not finite becomes NaN, and what is above 448 * 2^63 becomes 448 * 2^63.
  *

@@ -48,6 +48,11 @@ def least_scale(most):
     return 2.0 ** e
 
 
+def taken_scale(s):
+    """A stored scale as both operators take it."""
+    return min(max(s, 2.0 ** -32), 2.0 ** 63) if s == s else 2.0 ** -32
+
+
 def append(hit, app, tables, block_tokens, new, pool, scales=None):
     """new: [tokens, kv_heads, head_dim] (rotated already) into the pool, in place."""
     done = 0
@@ -66,7 +71,7 @@ def append(hit, app, tables, block_tokens, new, pool, scales=None):
                 v = v[np.isfinite(v)]
                 s = least_scale(v.max() if v.size else 0.0)
                 if row:
-                    old = float(scales[block, head])
+                    old = taken_scale(float(scales[block, head]))
                     s = max(s, old)
                     if s != old:
                         was = e4m3_values(pool[block, :row, head]) * (old / s)

@@ -205,7 +205,7 @@ __device__ __forceinline__ void append_codes(const AppendArgs &a, const AppendBl
     const uint32_t position = b.position, n = b.n * kHeadTasks, per = blockDim.x;
     float old[2];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) old[x] = b.row ? *planes[x].scale : 0.f;
+    for (int x = 0; x < 2; ++x) old[x] = b.row ? in_range(*planes[x].scale) : 0.f;
 
     auto load = [&](const CodesPlane &plane, uint32_t i, float (&e)[16]) {
         const uint32_t row = i / kHeadTasks;

@@ -36,7 +36,6 @@ struct AttnArgs {
     float c;                            // scale * log2(e)
 };
 
-constexpr float kLowestScale = 0x1p-32f, kHighestScale = 0x1p63f;
 // A row's maximum is raised, and what it has so far multiplied, only where a score is beyond it by more than this (in powers of two): weights
 // are then at most 2^8, which costs no bits, and most tiles raise nothing.
 constexpr float kSlack = 8.f;
@@ -100,7 +99,6 @@ __device__ __forceinline__ Scales load_scales(const AttnArgs &a, uint32_t block,
     const uint64_t at = (uint64_t)block * a.kv_heads + head;
     return {a.scale_k[at], a.scale_v[at]};
 }
-__device__ __forceinline__ float in_range(float scale) { return fminf(fmaxf(scale, kLowestScale), kHighestScale); }
 
 // Whether every query at positions [p0, p1] sees every key at places [v0, v1].
 __device__ __forceinline__ bool all_seen(const AttnArgs &a, const AttnItem &it, uint32_t v0, uint32_t v1, uint32_t p0, uint32_t p1) {

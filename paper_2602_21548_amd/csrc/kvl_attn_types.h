@@ -52,6 +52,9 @@ __device__ __forceinline__ uint32_t narrow(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), typename T::x2));
 }
 
+// The scale of a block and head, as both operators take it (NaN: the least).
+__device__ __forceinline__ float in_range(float scale) { return fminf(fmaxf(scale, 0x1p-32f), 0x1p63f); }
+
 // codes of e4m3, as floats
 template <int PAIR>
 __device__ __forceinline__ f32x2 widen_codes(uint32_t w) {
