@@ -65,7 +65,9 @@ typedef struct {
  * the hit prefix alone (what can be done before the new keys are there), KVL_TOKENS_APPEND the
  * appended tail, KVL_TOKENS_ALL both; KVL_HOST_ONLY, KVL_NO_POINTER_CHECKS and KVL_CALLER_SYNCS
  * as in kvl_plan.  KVL_ERANGE: a block id outside the pool, a table too short, a request of 2^31
- * tokens or more, 2^32 pool rows or new tokens or more; KVL_EALIAS: with KVL_SCATTER, a block
+ * tokens or more, 2^32 pool rows or new tokens or more, more work than a launch holds (2^24 pieces of attention
+ * work times cache heads, or as many workgroups that join them; with KVL_SCATTER and an 8-bit cache more than 2^23 blocks that
+ * receive new tokens times cache heads); KVL_EALIAS: with KVL_SCATTER, a block
  * that receives new tokens is named twice by the tables' receiving parts (requests may share the
  * blocks that they only read). */
 int kvl_attn_plan(const kvl_attn_layout_t *layout, const kvl_request_t *requests, uint32_t n_req,

@@ -230,8 +230,10 @@ static int build_attn(const kvl_attn_layout_t *layout, const kvl_request_t *req,
                 const uint32_t id = (uint32_t)req[r].block_table[b], n = (uint32_t)(upto - t);
                 if (taken[id] == stamp) return KVL_EALIAS;
                 taken[id] = stamp;
-                blocks.push_back({id, (uint32_t)(token0[r] + t - hit), (uint32_t)(t - b * bs), n, (uint32_t)t, {}});
-                plan->most_append_rows = std::max(plan->most_append_rows, n);
+                if (l.cache_dtype == KVL_E4M3) {        // (16-bit rows go by their tokens' places alone)
+                    blocks.push_back({id, (uint32_t)(token0[r] + t - hit), (uint32_t)(t - b * bs), n, (uint32_t)t, {}});
+                    plan->most_append_rows = std::max(plan->most_append_rows, n);
+                }
                 for (; t < upto; ++t) places.push_back({(uint32_t)t, (uint32_t)(id * bs + t - b * bs)});
             }
         }
