@@ -67,7 +67,7 @@ typedef struct {
  * as in kvl_plan.  KVL_ERANGE: a block id outside the pool, a table too short, a request of 2^31
  * tokens or more, 2^32 pool rows or new tokens or more, more work than a launch holds (2^24 pieces of attention
  * work times cache heads, or as many workgroups that join them; with KVL_SCATTER and an 8-bit cache more than 2^23 blocks that
- * receive new tokens times cache heads); KVL_EALIAS: with KVL_SCATTER, a block
+ * receive new tokens times cache heads, or new tokens beyond a block's row 2^28); KVL_EALIAS: with KVL_SCATTER, a block
  * that receives new tokens is named twice by the tables' receiving parts (requests may share the
  * blocks that they only read). */
 int kvl_attn_plan(const kvl_attn_layout_t *layout, const kvl_request_t *requests, uint32_t n_req,

@@ -95,6 +95,9 @@ static void merge_classes(const kvl_attn_layout_t &l, std::vector<Tile> &tiles) 
         if (t.cls != kRows128) t.cls = most;
 }
 
+// Rows of an 8-bit block up to its last new token: the append numbers them times 8 in 32 bits, with room for a step beyond the end.
+constexpr uint64_t kMostBlockRows = 1ull << 28;
+
 static int check_attn_layout(const kvl_attn_layout_t *l) {
     if (l->block_tokens == 0 || l->kv_heads == 0 || l->q_heads == 0 || l->q_heads % l->kv_heads) return KVL_EINVAL;
     if (l->q_heads > 65536) return KVL_EINVAL;
@@ -231,6 +234,7 @@ static int build_attn(const kvl_attn_layout_t *layout, const kvl_request_t *req,
                 if (taken[id] == stamp) return KVL_EALIAS;
                 taken[id] = stamp;
                 if (l.cache_dtype == KVL_E4M3) {        // (16-bit rows go by their tokens' places alone)
+                    if (upto - b * bs > kMostBlockRows) return KVL_ERANGE;
                     blocks.push_back({id, (uint32_t)(token0[r] + t - hit), (uint32_t)(t - b * bs), n, (uint32_t)t, {}});
                     plan->most_append_rows = std::max(plan->most_append_rows, n);
                 }

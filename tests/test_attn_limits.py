@@ -38,3 +38,15 @@ def test_pieces_of_attention():
     kw = dict(block_tokens=1, pool_blocks=1)
     refused([0] * n, [1] * n, [one] * n, K.KVL_GATHER | K.KVL_TOKENS_ALL, **kw)
     assert plan([0] * (n - 1), [1] * (n - 1), [one] * (n - 1), K.KVL_GATHER | K.KVL_TOKENS_ALL, **kw).tokens == n - 1
+
+
+def test_rows_of_an_8_bit_block():
+    """The kernel numbers a block's pieces of rows, up to eight each, in 32 bits."""
+    kw = dict(block_tokens=1 << 30, pool_blocks=3, kv_heads=1, q_heads=1, head_dim=128)
+    table = [np.array([2], dtype=np.int32)]
+    e4m3 = dict(cache_dtype=torch.float8_e4m3fn)
+    assert plan([(1 << 28) - 2], [2], table, K.KVL_SCATTER, **kw, **e4m3).tokens == 2
+    refused([(1 << 28) - 1], [2], table, K.KVL_SCATTER, **kw, **e4m3)
+    refused([(1 << 29) + 7], [1], table, K.KVL_SCATTER, **kw, **e4m3)
+    assert plan([(1 << 29) + 7], [1], table, K.KVL_SCATTER, **kw).tokens == 1
+    assert plan([(1 << 29) + 7], [1], table, K.KVL_GATHER | K.KVL_TOKENS_ALL, **kw, **e4m3).tokens == 1
