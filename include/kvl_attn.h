@@ -132,6 +132,7 @@ int kvl_append_layer(const kvl_attn_plan_t *plan, const kvl_append_t *args, void
  * logarithm of the sum of the exponentials, by which results over different ranges can be joined.
  * Scores, sums and outputs are held in 32 bits, softmax weights are rounded to dtype before they multiply values.
  * Keys that a query does not see do not reach its result, whatever they hold.  scale must be finite and positive.
+ * out may be q itself (with its stride); else out, lse and workspace must not overlap each other or what is read.
  * workspace: device memory of at least kvl_attn_plan_workspace bytes, 256-byte aligned, in nobody else's
  * use until the call's work is done.  With KVL_E4M3, scales are taken as at least 2^-32 and at most 2^63. */
 typedef struct {

@@ -210,7 +210,7 @@ def kvl_attn_layer(plan: AttnPlan, q: torch.Tensor, pool_planes: Sequence[torch.
                    lse: Optional[torch.Tensor] = None, stream=None) -> None:
     """Attention of the new tokens' queries over one layer's pool.
 
-    q, out: [tokens, q_heads, head_dim], tokens at a stride of their own; scale: 1 / sqrt(head_dim) by default; lse: float32
+    q, out: [tokens, q_heads, head_dim], tokens at a stride of their own; out may be q; scale: 1 / sqrt(head_dim) by default; lse: float32
     [tokens, q_heads], or None; workspace: a device tensor of plan.workspace_bytes (None if that is 0), in nobody else's use
     until the work is done."""
     what = "kvl_attn_layer"

@@ -40,6 +40,8 @@ static int attn_layer(const kvl_attn_plan_t *plan, const kvl_attn_t *in, const v
     const uint64_t n = plan->new_tokens, row = (uint64_t)l.q_heads * l.head_dim;
     if ((rc = check_rows(plan, t.q, n, row, &t.q_stride, true)) != KVL_OK) return rc;
     if ((rc = check_rows(plan, t.out, n, row, &t.out_stride, true)) != KVL_OK) return rc;
+    // (a row's queries are read by the workgroups of its tile alone, before the one or the join that writes it)
+    if (t.q == t.out && t.q_stride != t.out_stride) return KVL_EINVAL;
     if (t.lse) {
         uint64_t dense = 0;
         if (reinterpret_cast<uintptr_t>(t.lse) % 4) return KVL_EINVAL;
