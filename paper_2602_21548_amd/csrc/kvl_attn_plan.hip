@@ -294,7 +294,7 @@ int check_rows(const kvl_attn_plan_t *plan, const void *ptr, uint64_t n, uint64_
     if (*stride == 0) *stride = row;
     if (!ptr || *stride < row) return KVL_EINVAL;
     if (half && (reinterpret_cast<uintptr_t>(ptr) % 16 || *stride % 8)) return KVL_EINVAL;
-    if (*stride > (1ull << 40)) return KVL_EINVAL;
+    if (*stride > std::min<uint64_t>(1ull << 40, (1ull << 60) / n)) return KVL_EINVAL;     // (the extent is computed in 64 bits)
     return check_buffer(&plan->base, ptr, ((n - 1) * *stride + row) * (half ? 2 : 4), false);
 }
 

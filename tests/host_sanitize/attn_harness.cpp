@@ -296,9 +296,49 @@ static int check_append_launches() {
     return 0;
 }
 
+// A stride with which the last token would lie beyond what 64 bits number is refused, and does not come out as a small extent.
+static int check_strides() {
+    const uint32_t n = (1u << 23) + 1;
+    Batch b(1u << 24, 1, 1, 64, KVL_BF16);
+    b.add(0, n);
+    kvl_attn_plan_t *p = b.plan(KVL_SCATTER | KVL_GATHER | KVL_TOKENS_APPEND);
+    REQUIRE(p);
+    void *planes[2] = {somewhere(6), somewhere(7)};
+    const void *from[2] = {planes[0], planes[1]};
+    for (uint64_t stride : {1ull << 40, (1ull << 37) + 8, 1ull << 62, ~7ull}) {
+        uint64_t kvl_append_t::*strides[] = {&kvl_append_t::k_stride, &kvl_append_t::v_stride, &kvl_append_t::q_stride, &kvl_append_t::q_out_stride};
+        for (auto field : strides) {
+            kvl_append_t a{};
+            a.k = somewhere(1);
+            a.v = somewhere(2);
+            a.q = somewhere(3);
+            a.q_out = somewhere(4);
+            launches.clear();
+            REQUIRE(kvl_append_layer(p, &a, planes, fake::handle(s)) == KVL_OK && !launches.empty());
+            a.*field = stride;
+            launches.clear();
+            REQUIRE(kvl_append_layer(p, &a, planes, fake::handle(s)) == KVL_EINVAL && launches.empty());
+        }
+        for (bool out : {false, true}) {
+            kvl_attn_t a{};
+            a.q = somewhere(1);
+            a.out = somewhere(2);
+            a.scale = 1;
+            a.workspace = somewhere(3);
+            a.workspace_bytes = p->workspace_bytes;
+            (out ? a.out_stride : a.q_stride) = stride;
+            launches.clear();
+            REQUIRE(kvl_attn_layer(p, &a, from, fake::handle(s)) == KVL_EINVAL && launches.empty());
+        }
+    }
+    fake::finish(&s);
+    kvl_attn_plan_destroy(p);
+    return 0;
+}
+
 int main(int argc, char **argv) {
     const std::map<std::string, int (*)()> checks = {
-        {"lists", check_lists}, {"division", check_division}, {"classes", check_classes}, {"attn_launches", check_attn_launches}, {"append_launches", check_append_launches}};
+        {"lists", check_lists}, {"division", check_division}, {"classes", check_classes}, {"attn_launches", check_attn_launches}, {"append_launches", check_append_launches}, {"strides", check_strides}};
     if (argc != 2 || !checks.count(argv[1])) {
         for (const auto &c : checks) std::printf("%s\n", c.first.c_str());
         return argc == 1 ? 0 : 2;

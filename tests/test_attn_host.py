@@ -11,7 +11,7 @@ HERE = os.path.join(ROOT, "tests", "host_sanitize")
 ENV = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:verify_asan_link_order=0", UBSAN_OPTIONS="halt_on_error=1")
 ENV.pop("LD_PRELOAD", None)
 
-CHECKS = ["append_launches", "attn_launches", "classes", "division", "lists"]
+CHECKS = ["append_launches", "attn_launches", "classes", "division", "lists", "strides"]
 
 
 @pytest.fixture(scope="module")
