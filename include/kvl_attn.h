@@ -130,7 +130,9 @@ int kvl_append_layer(const kvl_attn_plan_t *plan, const kvl_append_t *args, void
  *   t <= p and (window == 0 or p - t < window or t < sinks), p the query's position.
  * A query that sees no key gets zeros (and lse -inf).  lse (optional, float [tokens][q_heads]): the natural
  * logarithm of the sum of the exponentials, by which results over different ranges can be joined.
- * Scores, sums and outputs are held in 32 bits, softmax weights are rounded to dtype before they multiply values.
+ * Scores, sums and outputs are held in 32 bits, softmax weights are rounded to dtype (or finer) before they multiply values.
+ * Over an 8-bit cache keys and values are c * scale exactly, but where scales are no powers of two and a request has more than
+ * 64 rows of queries (new tokens times q_heads / kv_heads): there they may be rounded to dtype once.
  * Keys that a query does not see do not reach its result, whatever they hold.  scale must be finite and positive.
  * out may be q itself (with its stride); else out, lse and workspace must not overlap each other or what is read.
  * workspace: device memory of at least kvl_attn_plan_workspace bytes, 256-byte aligned, in nobody else's

@@ -68,8 +68,9 @@ __device__ __forceinline__ u32x2 read_columns8(const char *at) {
 }
 
 // The item and head of a workgroup.  Workgroups go to the 8 XCDs in turn.  `TOGETHER`: the heads of one item, which lie side by side in
-// the rows of the pool, are taken by one XCD, one after the other.  That suits short pieces of rows (8-bit heads of 128, 64 requests of 16-64 K
-// tokens, 957 us against 1075) and not long ones (16-bit heads of 128 under a window of 4096, 376 us against 363).
+// the rows of the pool, are taken by one XCD, one after the other.  That suits heads whose part of a row is short, and not 256 bytes of it, whatever
+// the window (one new token, 64 + 8 heads; us together / apart; 32 requests of 16-64 K keys: 64 bytes 292 / 431, 128 of 8 bits 515 / 585, 128 of 16 bits 510 / 580,
+// 256 (24 of them) 684 / 663; 128 requests under a window of 4096: 115 / 164, 207 / 221, 204 / 217, 387 / 379).
 template <bool TOGETHER>
 __device__ __forceinline__ void place_of(uint32_t group, uint32_t groups, uint32_t heads, uint32_t *item, uint32_t *head) {
     if (TOGETHER && group < groups / (8 * heads) * (8 * heads)) {

@@ -17,7 +17,6 @@ typedef int i32x2 __attribute__((ext_vector_type(2)));
 // Half-precision element types: vectors, conversions and the matrix instructions that take them.
 struct Bf16 {
     typedef __bf16 x2 __attribute__((ext_vector_type(2)));
-    typedef __bf16 x4 __attribute__((ext_vector_type(4)));
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
     static constexpr uint32_t kExponent = 0x7f80u;
     static __device__ __forceinline__ f32x2 widen(uint32_t w) { return f32x2{__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)}; }
@@ -31,7 +30,6 @@ struct Bf16 {
 };
 struct F16 {
     typedef _Float16 x2 __attribute__((ext_vector_type(2)));
-    typedef _Float16 x4 __attribute__((ext_vector_type(4)));
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));
     static constexpr uint32_t kExponent = 0x7c00u;
     static __device__ __forceinline__ f32x2 widen(uint32_t w) {
