@@ -529,8 +529,8 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
 // bf16 numbers, the second one what the first leaves (their products with codes are exact, and a weight keeps 16 bits).
 //
 // The matrix instructions (37 % of the time busy) and the vector unit (46 %, most of it the exponentials and what goes with them) bound it, which
-// the two wavefronts that a SIMD has registers for do not overlap well: 850 TFLOP/s in 8-bit tails over long prefixes, heads of 128; of 64, 26 % and
-// 54 %, 630 under a window.
+// the two wavefronts that a SIMD has registers for do not overlap well: 810 to 850 TFLOP/s (by the card) in 8-bit tails over long prefixes, heads of 128; of 64,
+// 26 % and 55 %, 610 to 630 under a window.
 template <typename T, bool E4M3>
 __device__ __forceinline__ void codes_to_half(u32x4 w, float scale, u32x4 *x, u32x4 *y) {
     uint32_t e[8];
