@@ -72,6 +72,22 @@ typedef struct {
  * blocks that they only read). */
 int kvl_attn_plan(const kvl_attn_layout_t *layout, const kvl_request_t *requests, uint32_t n_req,
                   uint32_t flags, kvl_attn_plan_t **out);
+/* What the queries of one request see beside what the layout says.
+ * prefix: tokens [0, prefix) are seen by every query of the request, those before them too (as far as the plan's keys go), whatever
+ * the window.
+ * document_starts: host, ascending (KVL_EINVAL): the first tokens of documents; what is before the first of them is one, too.  A query sees keys
+ * of its own document only, and the prefix, and the layout's first tokens (sinks) that are not after it.
+ * So a query at position p sees token t if
+ *   t < prefix, or t <= p and (t < sinks, or (window == 0 or p - t < window) and t is in p's document). */
+typedef struct {
+    uint32_t prefix;
+    uint32_t n_documents;               /* 0: the request is one document */
+    const uint32_t *document_starts;    /* borrowed for the duration of the call */
+} kvl_attn_mask_t;
+/* kvl_attn_plan with a mask for each request (masks: host array of n_req, or NULL: none).  kvl_attn_layer and kvl_attn_scored_layer take the
+ * plan; what kvl_append_layer does with it is the same as without. */
+int kvl_attn_plan_masked(const kvl_attn_layout_t *layout, const kvl_request_t *requests, const kvl_attn_mask_t *masks,
+                         uint32_t n_req, uint32_t flags, kvl_attn_plan_t **out);
 /* As kvl_plan_destroy: does not wait for the device. */
 void kvl_attn_plan_destroy(kvl_attn_plan_t *plan);
 int kvl_attn_plan_tokens(const kvl_attn_plan_t *plan, uint64_t *new_tokens);
@@ -148,6 +164,38 @@ typedef struct {
     float scale;
 } kvl_attn_t;
 int kvl_attn_layer(const kvl_attn_plan_t *plan, const kvl_attn_t *args, const void *const *pool_planes, void *stream);
+
+/* kvl_attn_layer with other scores: in the place of s = scale * <q, K_t>
+ *   cap * tanh(s / cap)  where cap is not 0,  less  slopes[H] * |p - t|  where there are slopes (H: the query head).
+ * cap: 0, or from 2^-10 to 2^10 (KVL_EINVAL): a capped score is held to 2^-20 of the cap.  slopes: device, float [q_heads], or NULL; a bias and the score that it
+ * is added to are rounded to 32 bits, so that what a distant key's bias loses there is 2^-24 of the bias.
+ * scores: NULL for neither. */
+typedef struct {
+    float cap;
+    const float *slopes;
+} kvl_attn_scores_t;
+int kvl_attn_scored_layer(const kvl_attn_plan_t *plan, const kvl_attn_t *args, const kvl_attn_scores_t *scores,
+                          const void *const *pool_planes, void *stream);
+
+/* Results of attention over different keys, put together: with the lse of each,
+ *   lse = log sum_i exp(lses[i]),  out = sum_i exp(lses[i] - lse) parts[i]
+ * is what one call over all of the keys gives (for instance of a plan of the hit prefix and one of the appended tail; of ranges, pools or devices that
+ * each hold some of the keys).  A part whose lse is -inf has no share, whatever it holds; where all are, out is zeros and lse -inf.  Computed in 32 bits, rounded
+ * once.  A row with an lse that is +inf or NaN becomes NaN.
+ * The plan says how many tokens and heads of which type there are (a KVL_GATHER plan of the batch); its keys do not matter.
+ * Strides are in elements, 0 (or part_strides NULL): dense; multiples of 8; pointers of 16-bit rows 16-byte aligned (KVL_EINVAL).
+ * out may be one of the parts (with its stride) and lse one of the lses; else they must not overlap each other or what is read. */
+#define KVL_JOIN_MOST 16u
+typedef struct {
+    uint32_t n_parts;                   /* 1 .. KVL_JOIN_MOST */
+    const void *const *parts;           /* host array; each: device, [tokens][q_heads][head_dim] of dtype */
+    const uint64_t *part_strides;       /* host array, or NULL */
+    const float *const *lses;           /* host array; each: device, [tokens][q_heads] */
+    void *out;
+    uint64_t out_stride;
+    float *lse;                         /* or NULL */
+} kvl_attn_join_t;
+int kvl_attn_join(const kvl_attn_plan_t *plan, const kvl_attn_join_t *args, void *stream);
 
 #ifdef __cplusplus
 }

@@ -81,21 +81,32 @@ def append(hit, app, tables, block_tokens, new, pool, scales=None):
         done += int(n)
 
 
-def attend(hit, app, tables, block_tokens, q, k_pool, v_pool, scale, keys="all", window=0, sinks=0):
-    """q: [tokens, q_heads, head_dim]; pools of doubles.  Returns out, lse, and for each output what the rounding of softmax weights
-    can move: sum_t p_t |V_t|, and of each row the largest sum of |q K| over the keys."""
+def sees(p, t, window=0, sinks=0, prefix=0, starts=()):
+    """Whether the query at position p sees token t of its request."""
+    if t < prefix:
+        return True
+    if t > p:
+        return False
+    same = sum(x <= t for x in starts) == sum(x <= p for x in starts)
+    return t < sinks or (same and (not window or p - t < window))
+
+
+def attend(hit, app, tables, block_tokens, q, k_pool, v_pool, scale, keys="all", window=0, sinks=0, cap=0.0, slopes=None, prefix=None, documents=None):
+    """q: [tokens, q_heads, head_dim]; pools of doubles; prefix and documents: of each request.  Returns out, lse, and for each output what the rounding of
+    softmax weights can move: sum_t p_t |V_t|, and of each row the largest sum of |q K| over the keys."""
     tokens, q_heads, dim = q.shape
     kv_heads = k_pool.shape[2]
     group = q_heads // kv_heads
     out, lse = np.zeros(q.shape), np.full((tokens, q_heads), -np.inf)
     weight, reach = np.zeros(q.shape), np.zeros((tokens, q_heads))
     done = 0
-    for h, n, table in zip(hit, app, tables):
+    for r, (h, n, table) in enumerate(zip(hit, app, tables)):
         h, n = int(h), int(n)
+        mask = dict(window=window, sinks=sinks, prefix=0 if prefix is None else int(prefix[r]), starts=() if documents is None else documents[r])
         first, last = {"all": (0, h + n), "hit": (0, h), "append": (h, h + n)}[keys]
         for i in range(n):
             p = h + i
-            t = np.array([t for t in range(first, min(last, p + 1)) if not window or p - t < window or t < sinks], dtype=np.int64)
+            t = np.array([t for t in range(first, last) if sees(p, t, **mask)], dtype=np.int64)
             if not t.size:
                 continue
             blocks = np.asarray(table)[t // block_tokens]
@@ -103,6 +114,10 @@ def attend(hit, app, tables, block_tokens, q, k_pool, v_pool, scale, keys="all",
             for head in range(q_heads):
                 kh, vh, x = k[:, head // group], v[:, head // group], q[done + i, head]
                 s = scale * (kh @ x)
+                if cap:
+                    s = cap * np.tanh(s / cap)
+                if slopes is not None:
+                    s = s - float(slopes[head]) * np.abs(p - t)
                 top = s.max()
                 e = np.exp(s - top)
                 out[done + i, head] = (e @ vh) / e.sum()
@@ -111,3 +126,17 @@ def attend(hit, app, tables, block_tokens, q, k_pool, v_pool, scale, keys="all",
                 lse[done + i, head] = top + np.log(e.sum())
         done += n
     return out, lse, weight, reach
+
+
+def join(parts, lses):
+    """Results over different keys ([tokens, heads, dim] and [tokens, heads] each), put together."""
+    lses = np.array(lses, dtype=np.float64)
+    out, lse = np.zeros(np.shape(parts[0])), np.full(lses.shape[1:], -np.inf)
+    for at in np.ndindex(*lse.shape):
+        some = [i for i in range(len(parts)) if lses[i][at] != -np.inf]
+        if some:
+            top = max(lses[i][at] for i in some)
+            w = [np.exp(lses[i][at] - top) for i in some]
+            out[at] = sum(x * np.asarray(parts[i][at], dtype=np.float64) for x, i in zip(w, some)) / sum(w)
+            lse[at] = top + np.log(sum(w))
+    return out, lse

@@ -18,7 +18,7 @@ _EXPORTS = (
 )
 # attention over the loaded cache (include/kvl_attn.h)
 _ATTN_EXPORTS = (
-    "AttnPlan", "make_attn_layout", "kvl_attn_plan", "kvl_append_layer", "kvl_attn_layer",
+    "AttnPlan", "make_attn_layout", "kvl_attn_plan", "kvl_append_layer", "kvl_attn_layer", "kvl_attn_join", "KVL_JOIN_MOST",
     "KVL_BF16", "KVL_F16", "KVL_E4M3", "KVL_ROPE_HALVES", "KVL_ROPE_NEIGHBOURS",
 )
 __all__ = list(_EXPORTS + _ATTN_EXPORTS)

@@ -37,15 +37,33 @@ class kvl_attn_t(C.Structure):
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("scale", C.c_float)]
 
 
+class kvl_attn_mask_t(C.Structure):
+    _fields_ = [("prefix", C.c_uint32), ("n_documents", C.c_uint32), ("document_starts", C.POINTER(C.c_uint32))]
+
+
+class kvl_attn_scores_t(C.Structure):
+    _fields_ = [("cap", C.c_float), ("slopes", C.c_void_p)]
+
+
+class kvl_attn_join_t(C.Structure):
+    _fields_ = [("n_parts", C.c_uint32), ("parts", C.POINTER(C.c_void_p)), ("part_strides", C.POINTER(C.c_uint64)),
+                ("lses", C.POINTER(C.c_void_p)), ("out", C.c_void_p), ("out_stride", C.c_uint64), ("lse", C.c_void_p)]
+
+
+KVL_JOIN_MOST = 16
 _PLAN_P = C.c_void_p
 SIGNATURES = {
     "kvl_attn_plan": (C.c_int, [C.POINTER(kvl_attn_layout_t), C.POINTER(_b.kvl_request_t), C.c_uint32, C.c_uint32, C.POINTER(_PLAN_P)]),
+    "kvl_attn_plan_masked": (C.c_int, [C.POINTER(kvl_attn_layout_t), C.POINTER(_b.kvl_request_t), C.POINTER(kvl_attn_mask_t), C.c_uint32,
+                                       C.c_uint32, C.POINTER(_PLAN_P)]),
     "kvl_attn_plan_destroy": (None, [_PLAN_P]),
     "kvl_attn_plan_tokens": (C.c_int, [_PLAN_P, C.POINTER(C.c_uint64)]),
     "kvl_attn_plan_workspace": (C.c_int, [_PLAN_P, C.POINTER(C.c_uint64)]),
     "kvl_attn_plan_items": (C.c_int, [_PLAN_P, C.POINTER(kvl_attn_item_t), C.c_uint64, C.POINTER(C.c_uint64)]),
     "kvl_append_layer": (C.c_int, [_PLAN_P, C.POINTER(kvl_append_t), C.POINTER(C.c_void_p), C.c_void_p]),
     "kvl_attn_layer": (C.c_int, [_PLAN_P, C.POINTER(kvl_attn_t), C.POINTER(C.c_void_p), C.c_void_p]),
+    "kvl_attn_scored_layer": (C.c_int, [_PLAN_P, C.POINTER(kvl_attn_t), C.POINTER(kvl_attn_scores_t), C.POINTER(C.c_void_p), C.c_void_p]),
+    "kvl_attn_join": (C.c_int, [_PLAN_P, C.POINTER(kvl_attn_join_t), C.c_void_p]),
 }
 _lib = _b._lib
 for _name, (_res, _args) in SIGNATURES.items():
@@ -53,11 +71,11 @@ for _name, (_res, _args) in SIGNATURES.items():
     _fn.restype, _fn.argtypes = _res, _args
 
 if _b._native is not None:
-    _b._native.setup_attn(torch.float32, *(C.cast(getattr(_lib, f), C.c_void_p).value for f in ("kvl_append_layer", "kvl_attn_layer")))
+    _b._native.setup_attn(torch.float32, *(C.cast(getattr(_lib, f), C.c_void_p).value for f in ("kvl_append_layer", "kvl_attn_layer", "kvl_attn_scored_layer", "kvl_attn_join")))
     # (as binding.py's: what the library returned, or 1 for a call that is the general path's)
-    _fast_append, _fast_attn = _b._native.append_layer, _b._native.attn_layer
+    _fast_append, _fast_attn, _fast_join = _b._native.append_layer, _b._native.attn_layer, _b._native.attn_join
 else:
-    _fast_append = _fast_attn = _b._not_taken
+    _fast_append = _fast_attn = _fast_join = _b._not_taken
 
 
 def make_attn_layout(block_tokens: int, q_heads: int, kv_heads: int, head_dim: int, pool_blocks: int, dtype=torch.bfloat16,
@@ -135,12 +153,45 @@ class AttnPlan(_b._native.AttnPlanBase if _b._native is not None else object):
         return out
 
 
-def kvl_attn_plan(layout: kvl_attn_layout_t, hit, app, tables: Sequence[np.ndarray], flags: int) -> AttnPlan:
+def _masks(n: int, prefix, documents):
+    """(kvl_attn_mask_t array, arrays to keep alive while it is in use)"""
+    def checked(x, what):
+        x = np.asarray(x)
+        if x.ndim != 1 or (x.size and (x.dtype.kind not in "iu" or int(x.min()) < 0 or int(x.max()) >= 1 << 32)):
+            raise ValueError(f"kvl_attn_plan: {what} must be whole numbers from 0 to 2^32 - 1")
+        return np.ascontiguousarray(x, dtype=np.uint32)
+
+    masks, keep = (kvl_attn_mask_t * max(1, n))(), []
+    if prefix is not None:
+        prefix = checked(prefix, "prefix")
+        if prefix.size != n:
+            raise ValueError("kvl_attn_plan: prefix must have one entry per request")
+        for m, x in zip(masks, prefix.tolist()):
+            m.prefix = x
+    if documents is not None:
+        keep = [checked(d, "documents") for d in documents]
+        if len(keep) != n:
+            raise ValueError("kvl_attn_plan: documents must have one entry per request")
+        for m, d in zip(masks, keep):
+            m.n_documents = d.size
+            m.document_starts = d.ctypes.data_as(C.POINTER(C.c_uint32)) if d.size else None
+    return masks, keep
+
+
+def kvl_attn_plan(layout: kvl_attn_layout_t, hit, app, tables: Sequence[np.ndarray], flags: int, prefix=None,
+                  documents=None) -> AttnPlan:
     """One plan for both operators on a batch (hit prefix, appended tail and block table of each request, as kvl_plan):
-    KVL_SCATTER for kvl_append_layer, KVL_GATHER for kvl_attn_layer, with KVL_TOKENS_* for the keys that it sees."""
+    KVL_SCATTER for kvl_append_layer, KVL_GATHER for kvl_attn_layer, with KVL_TOKENS_* for the keys that it sees.
+
+    prefix: of each request, how many first tokens all of its queries see, those before them too.  documents: of each request, the ascending
+    first tokens of its documents; a query sees its own document (and the prefix, and the layout's sinks)."""
     reqs, n, _keep = _b._requests(hit, app, tables)
     out = C.c_void_p()
-    _b._check(_lib.kvl_attn_plan(C.byref(layout), reqs, n, flags, C.byref(out)), "kvl_attn_plan")
+    if prefix is None and documents is None:
+        _b._check(_lib.kvl_attn_plan(C.byref(layout), reqs, n, flags, C.byref(out)), "kvl_attn_plan")
+    else:
+        masks, _starts = _masks(n, prefix, documents)
+        _b._check(_lib.kvl_attn_plan_masked(C.byref(layout), reqs, masks, n, flags, C.byref(out)), "kvl_attn_plan_masked")
     return AttnPlan(out.value, layout, flags)
 
 
@@ -170,6 +221,12 @@ def _rows(plan: AttnPlan, t: torch.Tensor, shape, what: str):
     if per < dense or per % 8 or t.data_ptr() % 16:
         raise ValueError(f"{what}: tokens must lie at least {dense} elements apart, at multiples of 16 bytes")
     return t.data_ptr(), per
+
+
+def _lse(plan: AttnPlan, t: torch.Tensor, what: str) -> int:
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or tuple(t.shape) != plan._q_shape[:2]:
+        raise ValueError(f"{what}: must be float32 {plan._q_shape[:2]}")
+    return _b._dev(t, what)
 
 
 def kvl_append_layer(plan: AttnPlan, k: torch.Tensor, v: torch.Tensor, pool_planes: Sequence[torch.Tensor],
@@ -207,14 +264,19 @@ def kvl_append_layer(plan: AttnPlan, k: torch.Tensor, v: torch.Tensor, pool_plan
 
 def kvl_attn_layer(plan: AttnPlan, q: torch.Tensor, pool_planes: Sequence[torch.Tensor], out: torch.Tensor,
                    workspace: Optional[torch.Tensor] = None, scale: Optional[float] = None,
-                   lse: Optional[torch.Tensor] = None, stream=None) -> None:
+                   lse: Optional[torch.Tensor] = None, stream=None, cap: Optional[float] = None,
+                   slopes: Optional[torch.Tensor] = None) -> None:
     """Attention of the new tokens' queries over one layer's pool.
 
     q, out: [tokens, q_heads, head_dim], tokens at a stride of their own; out may be q; scale: 1 / sqrt(head_dim) by default; lse: float32
     [tokens, q_heads], or None; workspace: a device tensor of plan.workspace_bytes (None if that is 0), in nobody else's use
-    until the work is done."""
+    until the work is done.  cap: scores s become cap * tanh(s / cap) (None or 0: they stay); slopes: float32 [q_heads], scores lose
+    slopes[head] * |p - t|."""
     what = "kvl_attn_layer"
-    rc = _fast_attn(plan, q, pool_planes, out, workspace, scale, lse, stream)
+    if cap is None and slopes is None:
+        rc = _fast_attn(plan, q, pool_planes, out, workspace, scale, lse, stream)
+    else:
+        rc = _fast_attn(plan, q, pool_planes, out, workspace, scale, lse, stream, cap, slopes)
     if rc <= 0:
         return _b._check(rc, what)
     a = kvl_attn_t()
@@ -222,10 +284,38 @@ def kvl_attn_layer(plan: AttnPlan, q: torch.Tensor, pool_planes: Sequence[torch.
     a.q, a.q_stride = _rows(plan, q, plan._q_shape, f"{what} q")
     a.out, a.out_stride = _rows(plan, out, plan._q_shape, f"{what} out")
     if lse is not None:
-        if lse.dtype != torch.float32 or tuple(lse.shape) != plan._q_shape[:2]:
-            raise ValueError(f"{what}: lse must be float32 {plan._q_shape[:2]}")
-        a.lse = _b._dev(lse, f"{what} lse")
+        a.lse = _lse(plan, lse, f"{what} lse")
     if workspace is not None:
         a.workspace, a.workspace_bytes = _b._dev(workspace, f"{what} workspace"), workspace.nbytes
     a.scale = 1 / math.sqrt(plan.layout.head_dim) if scale is None else scale
-    _b._check(_lib.kvl_attn_layer(plan.handle, C.byref(a), arr, _b._stream_handle(stream)), what)
+    if cap is None and slopes is None:
+        return _b._check(_lib.kvl_attn_layer(plan.handle, C.byref(a), arr, _b._stream_handle(stream)), what)
+    scores = kvl_attn_scores_t(0 if cap is None else cap)
+    if slopes is not None:
+        if not isinstance(slopes, torch.Tensor) or slopes.dtype != torch.float32 or tuple(slopes.shape) != plan._q_shape[1:2]:
+            raise ValueError(f"{what}: slopes must be float32 {plan._q_shape[1:2]}")
+        scores.slopes = _b._dev(slopes, f"{what} slopes")
+    _b._check(_lib.kvl_attn_scored_layer(plan.handle, C.byref(a), C.byref(scores), arr, _b._stream_handle(stream)), what)
+
+
+def kvl_attn_join(plan: AttnPlan, parts: Sequence[torch.Tensor], lses: Sequence[torch.Tensor], out: torch.Tensor,
+                  lse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Results of attention over different keys (up to KVL_JOIN_MOST) put together, by the lse that kvl_attn_layer gave with each.
+
+    parts, out: [tokens, q_heads, head_dim] of the plan's type, tokens at a stride of their own; lses, lse: float32 [tokens, q_heads].
+    out may be one of the parts, lse one of the lses."""
+    what = "kvl_attn_join"
+    rc = _fast_join(plan, parts, lses, out, lse, stream)
+    if rc <= 0:
+        return _b._check(rc, what)
+    parts, lses = list(parts), list(lses)
+    n = len(parts)
+    if not 1 <= n <= KVL_JOIN_MOST or len(lses) != n:
+        raise ValueError(f"{what}: need 1 to {KVL_JOIN_MOST} parts, and an lse for each")
+    rows = [_rows(plan, t, plan._q_shape, f"{what} part") for t in parts]
+    a = kvl_attn_join_t(n, (C.c_void_p * n)(*(p for p, _ in rows)), (C.c_uint64 * n)(*(s for _, s in rows)),
+                        (C.c_void_p * n)(*(_lse(plan, t, f"{what} lse") for t in lses)))
+    a.out, a.out_stride = _rows(plan, out, plan._q_shape, f"{what} out")
+    if lse is not None:
+        a.lse = _lse(plan, lse, f"{what} lse")
+    _b._check(_lib.kvl_attn_join(plan.handle, C.byref(a), _b._stream_handle(stream)), what)

@@ -6,7 +6,9 @@ import os
 import subprocess
 import sys
 import sysconfig
+import tempfile
 import warnings
+from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
@@ -16,7 +18,7 @@ LIB = os.path.join(_HERE, "libkvl.so")
 NATIVE = os.path.join(_HERE, "_native" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 NATIVE_SOURCES = [os.path.join(_ROOT, "include", "kvl.h"), os.path.join(_ROOT, "include", "kvl_attn.h"), os.path.join(CSRC, "kvl_python.cpp")]
 SOURCES = ["kvl_plan.hip", "kvl_kernels.hip", "kvl_h2d.hip", "kvl_stream.hip", "kvl_noalloc.hip", "kvl_attn_plan.hip",
-           "kvl_append.hip", "kvl_attn.hip", "kvl_sched.cpp"]
+           "kvl_append.hip", "kvl_attn.hip", "kvl_attn_join.hip", "kvl_sched.cpp"]
 
 
 def hipcc() -> str:
@@ -62,23 +64,31 @@ def build_native(verbose: bool = False) -> str:
     return NATIVE
 
 
-def build(verbose: bool = False) -> str:
-    """Compile every source for gfx950 and link the shared library (always rebuilds)."""
-    cmd = [hipcc(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
-           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-           "-mllvm", "-amdgpu-kernarg-preload-count=14",       # scalar arguments of kernels in registers (see kvl_pack_quick_tile_kernel)
-           "-Wall", "-Wextra", "-Wno-unused-command-line-argument",
-           "-I" + os.path.join(_ROOT, "include"), "-I" + CSRC]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES]
-    tmp = LIB + f".tmp{os.getpid()}"
-    cmd += ["-o", tmp, "-Wl,-rpath,/opt/rocm/lib", "-Wl,--no-undefined"]
+def _run(cmd, verbose: bool) -> subprocess.CompletedProcess:
     if verbose:
         print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
+    return subprocess.run(cmd, capture_output=True, text=True)
+
+
+def build(verbose: bool = False) -> str:
+    """Compile every source for gfx950, side by side, and link the shared library (always rebuilds)."""
+    flags = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
+             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+             "-mllvm", "-amdgpu-kernarg-preload-count=14",       # scalar arguments of kernels in registers (see kvl_pack_quick_tile_kernel)
+             "-Wall", "-Wextra", "-Wno-unused-command-line-argument",
+             "-I" + os.path.join(_ROOT, "include"), "-I" + CSRC]
+    tmp = LIB + f".tmp{os.getpid()}"
+    with tempfile.TemporaryDirectory() as objects:
+        made = [os.path.join(objects, s + ".o") for s in SOURCES]
+        compile_ = [[hipcc(), *flags, "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, made)]
+        with ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+            done = list(pool.map(lambda cmd: _run(cmd, verbose), compile_))
+        if not any(r.returncode for r in done):
+            done.append(_run([hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", *made, "-o", tmp, "-Wl,-rpath,/opt/rocm/lib", "-Wl,--no-undefined"], verbose))
     # the host pass does not know the packed-fp32 feature switch and says so; that is harmless
     noise = ("packed-fp32-ops' is not a recognized feature", "'-packed-fp32-ops' is not")
-    err = "\n".join(l for l in res.stderr.splitlines() if not any(n in l for n in noise))
-    if res.returncode != 0:
+    err = "\n".join(l for r in done for l in r.stderr.splitlines() if not any(n in l for n in noise))
+    if any(r.returncode for r in done):
         if os.path.exists(tmp):
             os.unlink(tmp)
         raise RuntimeError("hipcc failed:\n" + err)

@@ -26,6 +26,14 @@ struct AttnItem {
 };
 static_assert(sizeof(AttnItem) == 48, "three descriptor units");
 
+// What a new token's queries see of their request: tokens [lo, hi), and those before `first` and `hi`.  Within a request lo and hi grow with the token,
+// and `first` is the same.
+struct AttnBounds {
+    uint32_t lo, hi, first;
+    uint32_t reserved;
+};
+static_assert(sizeof(AttnBounds) == 16, "a descriptor unit");
+
 // Rows whose keys were cut into pieces, for every cache head.
 struct JoinItem {
     uint32_t token0;
@@ -74,6 +82,8 @@ struct kvl_attn_plan_s {
     uint32_t class_first[kvl::kAttnClasses + 1] = {};   // items of each class
     uint32_t n_join = 0, most_join_rows = 0, most_pieces = 0, n_append_blocks = 0, most_append_rows = 0;
     uint64_t off_items = 0, off_join = 0, off_tables = 0, off_blocks = 0, off_tokens = 0;    // bytes into the device array
+    bool masked = false;                                // it has what each new token sees (kvl_attn_plan_masked):
+    uint64_t off_bounds = 0;                            // AttnBounds, there
     uint32_t div_mul = 0, div_shift = 0;                // t / block_tokens == 2 t * div_mul >> 32 + div_shift for t < 2^31
 
     // the join's wavefronts for each row, and its workgroups for each tile of rows and head

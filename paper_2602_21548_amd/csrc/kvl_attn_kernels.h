@@ -5,6 +5,9 @@
 // in one pass over the keys: m, l and the unnormalised output are kept for the keys so far, and what is there is multiplied by
 // 2^(m - m') where a tile raises m to m'.  Results over different keys are joined by the same rule.
 //
+// SCORED kernels take other scores, too: with s = <q, K_t>, log2(e) (cap tanh(scale s / cap) - slope |p - t|) in the place of c s, p the
+// query's position, and what a query sees from a list.  The others are the same code without that.
+//
 // The query heads that share a cache head are rows of one product: row = new token * group + head in group.
 //
 // Both kernels compute the scores' transpose, keys by rows of queries, S^T = K Q^T, and the outputs', O^T = V^T P^T.  In the
@@ -36,6 +39,21 @@ struct AttnArgs {
     float c;                            // scale * log2(e)
 };
 
+// What the SCORED kernels take beside that; c is 2 log2(e) scale / cap where there is a cap.
+struct ScoredArgs : AttnArgs {
+    const AttnBounds *bounds;           // of each new token; null: what the window leaves
+    const float *slopes;                // of each query head; null: none
+    float cap;                          // cap * log2(e); 0: none
+};
+template <bool SCORED>
+using ArgsOf = std::conditional_t<SCORED, ScoredArgs, AttnArgs>;
+
+// cap tanh(x / 2 log2(e)) with x = c s:  tanh(y) = 1 - 2 / (1 + e^(2 y)).  An infinite exponential gives the cap, none its negative.  (Beside
+// exact values it is off by some 2^-22 of the cap, whatever is left of a small tanh.)
+__device__ __forceinline__ float capped(float x, float cap) {
+    return __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x)), cap);
+}
+
 // A row's maximum is raised, and what it has so far multiplied, only where a score is beyond it by more than this (in powers of two): weights
 // are then at most 2^8, which costs no bits, and most tiles raise nothing.
 constexpr float kSlack = 8.f;
@@ -43,7 +61,7 @@ constexpr float kSlack = 8.f;
 template <typename T>
 constexpr float kLift = 0.f;
 template <>
-constexpr float kLift<F16> = 6.f;
+inline constexpr float kLift<F16> = 6.f;
 
 // The largest of the values of two lanes 32 apart, and of four lanes 16 apart.
 __device__ __forceinline__ float max_halves(float x) {
@@ -101,22 +119,57 @@ __device__ __forceinline__ Scales load_scales(const AttnArgs &a, uint32_t block,
     return {a.scale_k[at], a.scale_v[at]};
 }
 
-// Whether every query at positions [p0, p1] sees every key at places [v0, v1].
-__device__ __forceinline__ bool all_seen(const AttnArgs &a, const AttnItem &it, uint32_t v0, uint32_t v1, uint32_t p0, uint32_t p1) {
+// What a query sees: tokens t with lo <= t < hi, and those with t < first and t < hi.
+template <bool SCORED>
+__device__ __forceinline__ AttnBounds bounds_of(const ArgsOf<SCORED> &a, const AttnItem &it, uint32_t row) {
+    const uint32_t token = row / a.group, position = it.hit + token;
+    if constexpr (SCORED) {
+        if (a.bounds) return a.bounds[it.token0 + token];
+    }
+    return {position + 1 > a.window ? position + 1 - a.window : 0, position + 1, a.sinks, 0};
+}
+// The same of rows [row0, row1] of an item, both of whose ends grow with the row: the least and the greatest of each.
+struct RowsSee {
+    uint32_t lo0, lo1, hi0, hi1, first;
+};
+template <bool SCORED>
+__device__ __forceinline__ RowsSee rows_see(const ArgsOf<SCORED> &a, const AttnItem &it, uint32_t row0, uint32_t row1) {
+    const AttnBounds x = bounds_of<SCORED>(a, it, row0), y = bounds_of<SCORED>(a, it, row1);
+    return {x.lo, y.lo, x.hi, y.hi, x.first};
+}
+// Whether all of these rows see every key at places [v0, v1]; and whether none sees any.
+__device__ __forceinline__ bool all_seen(const AttnItem &it, const RowsSee &r, uint32_t v0, uint32_t v1) {
     const uint32_t t0 = v0 < it.sinks ? v0 : v0 + it.gap, t1 = v1 < it.sinks ? v1 : v1 + it.gap;
-    return v1 < it.end && t1 <= p0 && (t0 + a.window > p1 || t1 < a.sinks);
+    return v1 < it.end && t1 < r.hi0 && (t0 >= r.lo1 || t1 < r.first);
+}
+__device__ __forceinline__ bool none_seen(const AttnItem &it, const RowsSee &r, uint32_t v0, uint32_t v1) {
+    const uint32_t t0 = v0 < it.sinks ? v0 : v0 + it.gap, t1 = v1 < it.sinks ? v1 : v1 + it.gap;
+    return t0 >= r.hi1 || (t1 < r.lo0 && t0 >= r.first);
 }
 
-// The places that a query at `position` sees among those before `end`: v - first < count, and v < sinks.  (The first place whose token is t or a later
+// The places that a query sees among those before `end`: v - first < count, and v < sinks.  (The first place whose token is t or a later
 // one: t up to the first tokens' end, and t - gap beyond the gap.)
 struct Seen {
     uint32_t first, count, sinks;
     __device__ __forceinline__ bool operator()(uint32_t v) const { return (v - first < count) | (v < sinks); }
 };
-__device__ __forceinline__ Seen seen_from(const AttnArgs &a, const AttnItem &it, uint32_t position) {
+__device__ __forceinline__ Seen seen_from(const AttnItem &it, const AttnBounds &b) {
     auto place = [&](uint32_t t) { return t <= it.sinks ? t : max(t, it.sinks + it.gap) - it.gap; };
-    const uint32_t end = min(place(position + 1), it.end), first = place(position + 1 > a.window ? position + 1 - a.window : 0);
-    return {first, end > first ? end - first : 0, min(place(a.sinks), end)};
+    const uint32_t end = min(place(b.hi), it.end), first = place(b.lo);
+    return {first, end > first ? end - first : 0, min(place(b.first), end)};
+}
+
+// A row's bias: - slope |position - t|, slope times log2(e).
+struct Bias {
+    float slope;
+    uint32_t position;
+};
+__device__ __forceinline__ Bias bias_of(const ScoredArgs &a, const AttnItem &it, uint32_t head, uint32_t row) {
+    return {a.slopes ? 1.4426950408889634f * a.slopes[head * a.group + row % a.group] : 0.f, it.hit + row / a.group};
+}
+__device__ __forceinline__ float distance(const AttnItem &it, uint32_t place, uint32_t position) {
+    const int d = (int)(position - (place < it.sinks ? place : place + it.gap));
+    return (float)(d < 0 ? -d : d);
 }
 
 // Whether some of the elements in a word, two of T or four codes, are infinite or NaN; and the word with zeros for them.
@@ -221,8 +274,8 @@ __device__ __forceinline__ void write_lse(const AttnArgs &a, uint32_t token0, ui
 // Beyond 32 rows the registers do not hold a wavefront's outputs beside what is on its way, and scratch memory's loads come in order behind those of
 // the next keys: there HALVES = 2, and two wavefronts take the same tile of keys, half of the rows each; what the second one loads is in the caches.
 // (32 requests of 21 to 42 rows, 8-bit heads of 128: 59 us with three tiles of rows a wavefront and five such loads for each of keys, 51 so.)
-template <typename T, bool E4M3, int D, int RT, int HALVES>
-__global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) {
+template <typename T, bool E4M3, int D, int RT, int HALVES, bool SCORED = false>
+__global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const ArgsOf<SCORED> a) {
     constexpr int KT = few_rows_tile(D), NB = KT / 16;        // keys of a tile, blocks of 16
     constexpr int RB = D * (E4M3 ? 1 : 2);                          // bytes of a row
     constexpr int PR = RB / 16;                                     // pieces of 16 bytes in it
@@ -245,6 +298,7 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
     constexpr int kTiles = RT * HALVES;
     __shared__ x8 staged[kStaged ? kTiles * CH : 1][64];
     __shared__ Seen seen_of[kStaged ? kTiles * 16 : 1];
+    __shared__ Bias biases[SCORED && kStaged ? kTiles * 16 : 1];
 
     uint32_t item, head;
     place_of<(RB < 256)>(blockIdx.x, gridDim.x, a.kv_heads, &item, &head);
@@ -291,7 +345,7 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
         fetch(first);
     }
     x8 q[kStaged ? 1 : CH];
-    const uint32_t p0 = it.hit + it.first_row / a.group, p1 = it.hit + (it.first_row + it.n_rows - 1) / a.group;
+    const RowsSee see = rows_see<SCORED>(a, it, it.first_row, it.first_row + it.n_rows - 1);
 #pragma unroll
     for (int r = 0; r < kTiles; ++r) {
         const uint32_t i = min(r * 16 + n, it.n_rows - 1), row = it.first_row + i, token = row / a.group;
@@ -303,14 +357,20 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
             else if (wave == (uint32_t)(r * CH + s) % 4) staged[r * CH + s][lane] = *reinterpret_cast<const x8 *>(from + 2 * dim);
         }
     }
-    auto seen_by = [&](uint32_t i) { return seen_from(a, it, it.hit + (it.first_row + min(i, it.n_rows - 1)) / a.group); };
+    auto row_of = [&](uint32_t i) { return it.first_row + min(i, it.n_rows - 1); };
+    auto seen_by = [&](uint32_t i) { return seen_from(it, bounds_of<SCORED>(a, it, row_of(i))); };
     Seen seen_here{};
     if (!kStaged) seen_here = seen_by(n);
     else if (threadIdx.x < kTiles * 16) seen_of[threadIdx.x] = seen_by(threadIdx.x);
+    Bias bias_here{};
+    if constexpr (SCORED) {
+        if (!kStaged) bias_here = bias_of(a, it, head, row_of(n));
+        else if (threadIdx.x < kTiles * 16) biases[threadIdx.x] = bias_of(a, it, head, row_of(threadIdx.x));
+    }
     if (kStaged) __syncthreads();
     for (uint32_t tile = stream; tile < tiles; tile += kStreams) {
         const uint32_t v0 = it.begin + tile * KT;
-        const bool whole = all_seen(a, it, v0, v0 + KT - 1, p0, p1);
+        const bool whole = all_seen(it, see, v0, v0 + KT - 1);
         // Values that only some of the rows see must not reach the others: 0 * inf is NaN.  Infinities and NaN of such a tile are added
         // apart, to the rows that see them.
         const bool odd = !whole && __any(odd_pieces<T, E4M3>(vr));
@@ -379,7 +439,22 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const AttnArgs a) 
                     const f32x4 kc = E4M3 ? *reinterpret_cast<const f32x4 *>(key_c + at_key) : f32x4{a.c, a.c, a.c, a.c};
                     const f32x4 kl = E4M3 ? *reinterpret_cast<const f32x4 *>(key_log + at_key) : f32x4{0, 0, 0, 0};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) s[r][b][i] = E4M3 ? __builtin_fmaf(s[r][b][i], kc[i], kl[i]) : s[r][b][i] * kc[i];
+                    for (int i = 0; i < 4; ++i) {
+                        const float x = s[r][b][i];
+                        s[r][b][i] = E4M3 ? __builtin_fmaf(x, kc[i], kl[i]) : x * kc[i];
+                        if constexpr (SCORED) {
+                            if (a.cap != 0.f) s[r][b][i] = capped(x * kc[i], a.cap) + (E4M3 ? kl[i] : 0.f);
+                        }
+                    }
+                }
+                if constexpr (SCORED) {
+                    if (a.slopes) {
+                        const Bias bias = kStaged ? biases[((R0 + r) * HALVES + half) * 16 + n] : bias_here;
+#pragma unroll
+                        for (int b = 0; b < NB; ++b)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) s[r][b][i] -= bias.slope * distance(it, v0 + 16 * b + 4 * g + i, bias.position);
+                    }
                 }
                 if (!whole) {
                     const Seen seen = kStaged ? seen_of[((R0 + r) * HALVES + half) * 16 + n] : seen_here;
@@ -555,8 +630,8 @@ __device__ __forceinline__ void codes_to_half(u32x4 w, float scale, u32x4 *x, u3
 // Scales that leave codes in fp16's range.
 __device__ __forceinline__ bool suits_f16(float scale) { return scale >= 0x1p-15f && scale <= 0x1p7f; }
 
-template <typename T, bool E4M3, int D>
-__global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(const AttnArgs a) {
+template <typename T, bool E4M3, int D, bool SCORED = false>
+__global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(const ArgsOf<SCORED> a) {
     constexpr int KT = kManyRowsTile;
     constexpr int RB = 2 * D;                                       // bytes of a row in the LDS
     constexpr int PR = D * (E4M3 ? 1 : 2) / 16;                     // pieces of a row in memory
@@ -583,10 +658,12 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
     const uint32_t rows_before = wave * 32;
     const bool works = rows_before < it.n_rows;
     const uint32_t row = it.first_row + min(rows_before + n, it.n_rows - 1);
-    const uint32_t p0 = it.hit + it.first_row / a.group, p1 = it.hit + (it.first_row + it.n_rows - 1) / a.group;
-    const uint32_t w0 = it.hit + (it.first_row + min(rows_before, it.n_rows - 1)) / a.group,
-                   w1 = it.hit + (it.first_row + min(rows_before + 31, it.n_rows - 1)) / a.group;
-    const Seen seen = seen_from(a, it, it.hit + row / a.group);
+    // what the workgroup's rows see, and the wavefront's
+    const RowsSee all_see = rows_see<SCORED>(a, it, it.first_row, it.first_row + it.n_rows - 1);
+    const RowsSee see = rows_see<SCORED>(a, it, it.first_row + min(rows_before, it.n_rows - 1), it.first_row + min(rows_before + 31, it.n_rows - 1));
+    const Seen seen = seen_from(it, bounds_of<SCORED>(a, it, row));
+    Bias bias{};
+    if constexpr (SCORED) bias = bias_of(a, it, head, row);
     x8 q[CH];
     {
         const char *from = a.q + 2 * ((it.token0 + row / a.group) * a.q_stride + (head * a.group + row % a.group) * D);
@@ -629,7 +706,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
         const uint32_t v0 = it.begin + tile * KT;
         char *k_lds = lds[tile % 2][0], *v_lds = lds[tile % 2][1];
         // (infinities and NaN among values that not all rows see: as in the kernel above)
-        if (!all_seen(a, it, v0, v0 + KT - 1, p0, p1) && odd_pieces<T, E4M3>(vr)) {
+        if (!all_seen(it, all_see, v0, v0 + KT - 1) && odd_pieces<T, E4M3>(vr)) {
             odd_tile[tile % 3] = 1;
             make_plain<T, E4M3>(vr);
         }
@@ -674,10 +751,8 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
 
         asm volatile("" : "+v"(k_at), "+v"(v_at));      // (the addresses made of them are made anew for each tile: registers are short)
         // a tile that none of the wavefront's rows sees
-        const uint32_t v1 = min(v0 + KT, it.end) - 1;
-        const uint32_t t0 = v0 < it.sinks ? v0 : v0 + it.gap, t1 = v1 < it.sinks ? v1 : v1 + it.gap;
-        if (!works || t0 > w1 || (t1 + a.window <= w0 && t0 >= a.sinks)) continue;
-        const bool whole = all_seen(a, it, v0, v0 + KT - 1, w0, w1);
+        if (!works || none_seen(it, see, v0, min(v0 + KT, it.end) - 1)) continue;
+        const bool whole = all_seen(it, see, v0, v0 + KT - 1);
 
         // scores: lane (n, h) gets row n's of keys 32 b + 8 (i / 4) + 4 h + i % 4
         f32x16 s[2];
@@ -703,6 +778,24 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[b][i] *= of_key(by.k, 32 * b + 8 * (i / 4) + i % 4);
         }
+        float c = a.c;
+        if constexpr (SCORED) {                     // (scores that are made anew are in powers of two from there on)
+            if (a.cap != 0.f) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[b][i] = capped(s[b][i] * c, a.cap);
+                c = 1.f;
+            }
+            if (a.slopes) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        s[b][i] = __builtin_fmaf(s[b][i], c, -bias.slope * distance(it, v0 + 4 * h + 32 * b + 8 * (i / 4) + i % 4, bias.position));
+                c = 1.f;
+            }
+        }
         if (!whole) {
 #pragma unroll
             for (int b = 0; b < 2; ++b)
@@ -716,7 +809,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-        top = max_halves(top) * a.c;
+        top = max_halves(top) * c;
         if (__any(top > m + kSlack)) {
             const float to = fmaxf(m, top), f = factor(m, to);
             m = to;
@@ -729,8 +822,8 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
         const float from = m == -__builtin_inff() ? 0.f : kLift<T> - m;
         // the weights of keys 16 u + 8 (i / 4) + 4 h + i % 4 and the next, i even
         auto weights = [&](int u, int i) {
-            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u / 2][8 * (u % 2) + i], a.c, from));
-            const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u / 2][8 * (u % 2) + i + 1], a.c, from));
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u / 2][8 * (u % 2) + i], c, from));
+            const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u / 2][8 * (u % 2) + i + 1], c, from));
             l += x + y;
             return f32x2{x, y};
         };

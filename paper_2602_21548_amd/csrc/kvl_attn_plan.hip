@@ -18,12 +18,25 @@ struct Tile {
 };
 }  // namespace
 
-// Keys [first, last) of the plan, queries at positions [p0, p1]: what at least one of them sees.
-static Places places_of(const kvl_attn_layout_t &l, uint64_t first, uint64_t last, uint64_t p0, uint64_t p1) {
-    const uint64_t end = std::max(first, std::min(last, p1 + 1));
-    uint64_t lo = first;
-    if (l.window) lo = std::min(end, std::max(first, p0 + 1 > l.window ? p0 + 1 - l.window : 0));
-    const uint64_t sinks = std::max(first, std::min<uint64_t>(l.sinks, lo));
+// What the query at position p of a request sees (AttnBounds).
+static AttnBounds bounds_of(const kvl_attn_layout_t &l, const kvl_attn_mask_t *mask, uint64_t p) {
+    uint64_t lo = l.window && p + 1 > l.window ? p + 1 - l.window : 0, hi = p + 1;
+    uint32_t first = l.sinks;
+    if (mask) {
+        const uint32_t *starts = mask->document_starts, *next = std::upper_bound(starts, starts + mask->n_documents, p);
+        if (next != starts) lo = std::max<uint64_t>(lo, next[-1]);
+        hi = std::max<uint64_t>(hi, mask->prefix);
+        first = std::max(first, mask->prefix);
+    }
+    return {(uint32_t)lo, (uint32_t)hi, first, 0};
+}
+
+// Keys [first, last) of the plan, of which the first query sees what x says and the last one what y says: what at least one of the queries from
+// that to this sees.
+static Places places_of(uint64_t first, uint64_t last, const AttnBounds &x, const AttnBounds &y) {
+    const uint64_t end = std::max(first, std::min<uint64_t>(last, y.hi));
+    const uint64_t lo = std::min(end, std::max<uint64_t>(first, x.lo));
+    const uint64_t sinks = std::max(first, std::min<uint64_t>(x.first, lo));
     return {(uint32_t)first, (uint32_t)(sinks + end - lo), (uint32_t)sinks, (uint32_t)(lo - sinks)};
 }
 
@@ -115,8 +128,8 @@ static void put(std::vector<kvl_unit_t> &blob, uint64_t at, const void *from, si
     if (bytes) std::memcpy(reinterpret_cast<char *>(blob.data()) + at, from, bytes);
 }
 
-static int build_attn(const kvl_attn_layout_t *layout, const kvl_request_t *req, uint32_t n_req, uint32_t flags,
-                      kvl_attn_plan_t *plan) {
+static int build_attn(const kvl_attn_layout_t *layout, const kvl_request_t *req, const kvl_attn_mask_t *masks, uint32_t n_req,
+                      uint32_t flags, kvl_attn_plan_t *plan) {
     const kvl_attn_layout_t &l = *layout;
     const uint64_t bs = l.block_tokens;
     const uint32_t group = l.q_heads / l.kv_heads;
@@ -142,6 +155,12 @@ static int build_attn(const kvl_attn_layout_t *layout, const kvl_request_t *req,
         if (blocks && !req[r].block_table) return KVL_EINVAL;
         for (uint64_t b = 0; b < blocks; ++b)
             if (req[r].block_table[b] < 0 || (uint64_t)req[r].block_table[b] >= l.pool_blocks) return KVL_ERANGE;
+        if (masks) {
+            const kvl_attn_mask_t &m = masks[r];
+            if (m.n_documents && !m.document_starts) return KVL_EINVAL;
+            for (uint32_t d = 1; d < m.n_documents; ++d)
+                if (m.document_starts[d] <= m.document_starts[d - 1]) return KVL_EINVAL;
+        }
         token0[r] = tokens;
         table0[r] = entries;
         tokens += n;
@@ -163,7 +182,8 @@ static int build_attn(const kvl_attn_layout_t *layout, const kvl_request_t *req,
             const uint32_t c = rows <= 16 ? kRows16 : rows <= 32 ? kRows32 : rows <= 64 ? kRows64 : kRows128;
             for (uint64_t r0 = 0; r0 < rows; r0 += kClassRows[c]) {
                 const uint64_t r1 = std::min<uint64_t>(rows, r0 + kClassRows[c]);
-                const Places at = places_of(l, first, last, hit + r0 / group, hit + (r1 - 1) / group);
+                const kvl_attn_mask_t *mask = masks ? masks + r : nullptr;
+                const Places at = places_of(first, last, bounds_of(l, mask, hit + r0 / group), bounds_of(l, mask, hit + (r1 - 1) / group));
                 tiles.push_back({r, (uint32_t)r0, (uint32_t)(r1 - r0), c, at});
             }
         }
@@ -255,6 +275,13 @@ static int build_attn(const kvl_attn_layout_t *layout, const kvl_request_t *req,
             tables.insert(tables.end(), req[r].block_table, req[r].block_table + n);
         }
     }
+    std::vector<AttnBounds> bounds;
+    if (masks && (flags & KVL_GATHER)) {
+        plan->masked = true;
+        bounds.reserve(tokens);
+        for (uint32_t r = 0; r < n_req; ++r)
+            for (uint64_t i = 0; i < req[r].append_tokens; ++i) bounds.push_back(bounds_of(l, masks + r, (uint64_t)req[r].hit_tokens + i));
+    }
     uint64_t at = 0;
     auto room = [&at](uint64_t bytes) {
         const uint64_t here = at;
@@ -266,6 +293,7 @@ static int build_attn(const kvl_attn_layout_t *layout, const kvl_request_t *req,
     plan->off_tables = room(tables.size() * sizeof(int32_t));
     plan->off_blocks = room(blocks.size() * sizeof(AppendBlock));
     plan->off_tokens = room(places.size() * sizeof(AppendToken));
+    plan->off_bounds = room(bounds.size() * sizeof(AttnBounds));
     if (flags & KVL_HOST_ONLY) return KVL_OK;
     plan->base.units.resize(at / 16);
     put(plan->base.units, plan->off_items, items.data(), items.size() * sizeof(AttnItem));
@@ -273,6 +301,7 @@ static int build_attn(const kvl_attn_layout_t *layout, const kvl_request_t *req,
     put(plan->base.units, plan->off_tables, tables.data(), tables.size() * sizeof(int32_t));
     put(plan->base.units, plan->off_blocks, blocks.data(), blocks.size() * sizeof(AppendBlock));
     put(plan->base.units, plan->off_tokens, places.data(), places.size() * sizeof(AppendToken));
+    put(plan->base.units, plan->off_bounds, bounds.data(), bounds.size() * sizeof(AttnBounds));
     const int rc = upload_units(&plan->base);
     std::vector<kvl_unit_t>().swap(plan->base.units);       // (it is on the device now)
     return rc;
@@ -305,6 +334,11 @@ int check_rows(const kvl_attn_plan_t *plan, const void *ptr, uint64_t n, uint64_
 extern "C" {
 
 int kvl_attn_plan(const kvl_attn_layout_t *layout, const kvl_request_t *requests, uint32_t n_req, uint32_t flags, kvl_attn_plan_t **out) {
+    return kvl_attn_plan_masked(layout, requests, nullptr, n_req, flags, out);
+}
+
+int kvl_attn_plan_masked(const kvl_attn_layout_t *layout, const kvl_request_t *requests, const kvl_attn_mask_t *masks, uint32_t n_req,
+                         uint32_t flags, kvl_attn_plan_t **out) {
     if (!layout || !out || (n_req && !requests)) return KVL_EINVAL;
     *out = nullptr;
     if (!(flags & (KVL_GATHER | KVL_SCATTER))) return KVL_EINVAL;
@@ -316,7 +350,7 @@ int kvl_attn_plan(const kvl_attn_layout_t *layout, const kvl_request_t *requests
     kvl_attn_plan_t *plan = new (std::nothrow) kvl_attn_plan_t;
     if (!plan) return KVL_ENOMEM;
     try {
-        rc = kvl::build_attn(layout, requests, n_req, flags, plan);
+        rc = kvl::build_attn(layout, requests, masks, n_req, flags, plan);
     } catch (const std::exception &) {                      // (bad_alloc, length_error)
         rc = KVL_ENOMEM;
     }

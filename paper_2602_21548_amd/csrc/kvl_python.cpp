@@ -48,6 +48,8 @@ struct Library {
     decltype(&kvl_pool_to_fullblocks_layer) to_blocks;
     decltype(&kvl_append_layer) append;
     decltype(&kvl_attn_layer) attn;
+    decltype(&kvl_attn_scored_layer) scored;
+    decltype(&kvl_attn_join) join;
 } g_lib;
 PyObject *g_float32;
 PyObject *g_tensor_type, *g_array_type, *g_raw_stream, *g_get_device, *g_is_initialized;
@@ -303,8 +305,18 @@ PyObject *append_layer(PyObject *, PyObject *const *a, Py_ssize_t n) {  // plan,
     KVL_CALL(g_lib.append((const kvl_attn_plan_t *)handle, &t, planes, s));
 }
 
-PyObject *attn_layer(PyObject *, PyObject *const *a, Py_ssize_t n) {    // plan, q, pool planes, out, workspace, scale, lse, stream
-    AttnPlanObject *plan = n == 8 ? attn_plan_of(a[0]) : nullptr;
+// float32 [tokens, q_heads]
+bool lse_of(AttnPlanObject *plan, PyObject *o, float **ptr) {
+    Buffer b;
+    unsigned long long shape[2];
+    if (!buffer(o, false, &b) || !is_type(o, g_float32) || !numbers(PyObject_GetAttr(o, s_shape), 2, shape)) return false;
+    *ptr = (float *)b.ptr;
+    return shape[0] == plan->tokens && shape[1] == plan->q_heads;
+}
+
+// plan, q, pool planes, out, workspace, scale, lse, stream; and cap, slopes
+PyObject *attn_layer(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    AttnPlanObject *plan = n == 8 || n == 10 ? attn_plan_of(a[0]) : nullptr;
     void *planes[kAttnPlanes], *s;
     const void *to;
     kvl_attn_t t{};
@@ -320,16 +332,55 @@ PyObject *attn_layer(PyObject *, PyObject *const *a, Py_ssize_t n) {    // plan,
     if (a[5] == Py_None) t.scale = plan->scale;
     else if (PyFloat_CheckExact(a[5])) t.scale = (float)PyFloat_AS_DOUBLE(a[5]);
     else KVL_NOT_TAKEN;
-    if (a[6] != Py_None) {
-        Buffer b;
-        unsigned long long shape[2];
-        if (!buffer(a[6], false, &b) || !is_type(a[6], g_float32) || !numbers(PyObject_GetAttr(a[6], s_shape), 2, shape)) KVL_NOT_TAKEN;
-        if (shape[0] != plan->tokens || shape[1] != plan->q_heads) KVL_NOT_TAKEN;
-        t.lse = (float *)b.ptr;
+    if (a[6] != Py_None && !lse_of(plan, a[6], &t.lse)) KVL_NOT_TAKEN;
+    kvl_attn_scores_t scores{};
+    if (n == 10) {
+        if (PyFloat_CheckExact(a[8])) scores.cap = (float)PyFloat_AS_DOUBLE(a[8]);
+        else if (a[8] != Py_None) KVL_NOT_TAKEN;
+        if (a[9] != Py_None) {
+            Buffer b;
+            unsigned long long shape[1];
+            if (!buffer(a[9], false, &b) || !is_type(a[9], g_float32) || !numbers(PyObject_GetAttr(a[9], s_shape), 1, shape)) KVL_NOT_TAKEN;
+            if (shape[0] != plan->q_heads) KVL_NOT_TAKEN;
+            scores.slopes = (const float *)b.ptr;
+        }
     }
     if (!stream(a[7], &s) || !plan->handle) KVL_NOT_TAKEN;
     void *handle = plan->handle;
+    if (n == 10) KVL_CALL(g_lib.scored((const kvl_attn_plan_t *)handle, &t, &scores, planes, s));
     KVL_CALL(g_lib.attn((const kvl_attn_plan_t *)handle, &t, planes, s));
+}
+
+PyObject *attn_join(PyObject *, PyObject *const *a, Py_ssize_t n) {     // plan, parts, lses, out, lse, stream
+    AttnPlanObject *plan = n == 6 ? attn_plan_of(a[0]) : nullptr;
+    if (!plan || !PyList_CheckExact(a[1]) || !PyList_CheckExact(a[2])) KVL_NOT_TAKEN;
+    const Py_ssize_t parts = PyList_GET_SIZE(a[1]);
+    if (parts < 1 || parts > (Py_ssize_t)KVL_JOIN_MOST || PyList_GET_SIZE(a[2]) != parts) KVL_NOT_TAKEN;
+    const void *from[KVL_JOIN_MOST], *to;
+    float *lses[KVL_JOIN_MOST];
+    uint64_t strides[KVL_JOIN_MOST];
+    void *s;
+    kvl_attn_join_t t{};
+    for (Py_ssize_t i = 0; i < parts; ++i) {
+        if (PyList_GET_SIZE(a[1]) != parts || PyList_GET_SIZE(a[2]) != parts) KVL_NOT_TAKEN;       // (as in pool())
+        PyObject *part = PyList_GET_ITEM(a[1], i), *lse = PyList_GET_ITEM(a[2], i);
+        Py_INCREF(part);
+        Py_INCREF(lse);
+        const bool ok = rows_of(plan, part, plan->q_heads, &from[i], &strides[i]) && lse_of(plan, lse, &lses[i]);
+        Py_DECREF(part);
+        Py_DECREF(lse);
+        if (!ok) KVL_NOT_TAKEN;
+    }
+    if (!rows_of(plan, a[3], plan->q_heads, &to, &t.out_stride)) KVL_NOT_TAKEN;
+    if (a[4] != Py_None && !lse_of(plan, a[4], &t.lse)) KVL_NOT_TAKEN;
+    if (!stream(a[5], &s) || !plan->handle) KVL_NOT_TAKEN;
+    void *handle = plan->handle;
+    t.n_parts = (uint32_t)parts;
+    t.parts = from;
+    t.part_strides = strides;
+    t.lses = lses;
+    t.out = const_cast<void *>(to);
+    KVL_CALL(g_lib.join((const kvl_attn_plan_t *)handle, &t, s));
 }
 
 // requests(hit, app, tables, out): a batch's kvl_request_t into `out`, from contiguous uint32 arrays and a list of contiguous
@@ -403,15 +454,17 @@ PyObject *setup(PyObject *, PyObject *args) {
     Py_RETURN_NONE;
 }
 
-// setup_attn(torch.float32, the addresses of the attention operators' two entry points)
+// setup_attn(torch.float32, the addresses of the attention operators' four entry points)
 PyObject *setup_attn(PyObject *, PyObject *args) {
     PyObject *type;
-    unsigned long long f[2];
-    if (!PyArg_ParseTuple(args, "OKK", &type, &f[0], &f[1])) return nullptr;
+    unsigned long long f[4];
+    if (!PyArg_ParseTuple(args, "OKKKK", &type, &f[0], &f[1], &f[2], &f[3])) return nullptr;
     Py_INCREF(type);
     g_float32 = type;
     g_lib.append = (decltype(g_lib.append))(uintptr_t)f[0];
     g_lib.attn = (decltype(g_lib.attn))(uintptr_t)f[1];
+    g_lib.scored = (decltype(g_lib.scored))(uintptr_t)f[2];
+    g_lib.join = (decltype(g_lib.join))(uintptr_t)f[3];
     Py_RETURN_NONE;
 }
 
@@ -524,6 +577,7 @@ PyMethodDef module_methods[] = {
     {"pool_to_fullblocks_layer", (PyCFunction)(void (*)(void))pool_to_fullblocks_layer, METH_FASTCALL, nullptr},
     {"append_layer", (PyCFunction)(void (*)(void))append_layer, METH_FASTCALL, nullptr},
     {"attn_layer", (PyCFunction)(void (*)(void))attn_layer, METH_FASTCALL, nullptr},
+    {"attn_join", (PyCFunction)(void (*)(void))attn_join, METH_FASTCALL, nullptr},
     {"requests", (PyCFunction)(void (*)(void))requests, METH_FASTCALL, nullptr},
     {"setup", setup, METH_VARARGS, nullptr},
     {"setup_attn", setup_attn, METH_VARARGS, nullptr},
