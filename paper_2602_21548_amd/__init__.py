@@ -21,13 +21,18 @@ _ATTN_EXPORTS = (
     "AttnPlan", "make_attn_layout", "kvl_attn_plan", "kvl_append_layer", "kvl_attn_layer", "kvl_attn_join", "KVL_JOIN_MOST",
     "KVL_BF16", "KVL_F16", "KVL_E4M3", "KVL_ROPE_HALVES", "KVL_ROPE_NEIGHBOURS",
 )
-__all__ = list(_EXPORTS + _ATTN_EXPORTS)
+# whose the cache's blocks are (include/kvl_pages.h)
+_PAGES_EXPORTS = (
+    "Pages", "PagePools", "kvl_pages", "kvl_pages_adopt", "kvl_pages_fork", "kvl_pages_extend", "kvl_pages_truncate", "kvl_pages_free",
+    "kvl_pages_compact", "kvl_pages_tables", "kvl_pages_tokens", "kvl_pages_stats", "kvl_page_pools", "kvl_copy_blocks",
+)
+__all__ = list(_EXPORTS + _ATTN_EXPORTS + _PAGES_EXPORTS)
 
 
 def __getattr__(name):
     if name in __all__:
         # found here from now on: coming by this way took 3.6 us of every call
-        module = ".binding" if name in _EXPORTS else ".attn"
+        module = ".binding" if name in _EXPORTS else ".attn" if name in _ATTN_EXPORTS else ".pages"
         value = globals()[name] = getattr(importlib.import_module(module, __name__), name)
         return value
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
