@@ -104,6 +104,7 @@ static int attn_layer(const kvl_attn_plan_t *plan, const kvl_attn_t *in, const k
         a.c = std::fmin(2 * a.c / how.cap, 0x1p126f);
         a.cap = how.cap * 1.4426950408889634f;
     }
+    a.over = 1 / (a.cap != 0 ? 2 * a.cap : a.c);
     a.slopes = how.slopes;
     if (plan->masked) a.bounds = reinterpret_cast<const AttnBounds *>(reinterpret_cast<const char *>(plan->base.d_units) + plan->off_bounds);
     AttnLaunch go(plan, stream);

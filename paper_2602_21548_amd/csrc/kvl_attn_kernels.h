@@ -44,15 +44,15 @@ struct ScoredArgs : AttnArgs {
     const AttnBounds *bounds;           // of each new token; null: what the window leaves
     const float *slopes;                // of each query head; null: none
     float cap;                          // cap * log2(e); 0: none
+    float over;                         // 1 / (2 cap), without a cap 1 / c
 };
 template <bool SCORED>
 using ArgsOf = std::conditional_t<SCORED, ScoredArgs, AttnArgs>;
 
-// cap tanh(x / 2 log2(e)) with x = c s:  tanh(y) = 1 - 2 / (1 + e^(2 y)).  An infinite exponential gives the cap, none its negative.  (Beside
-// exact values it is off by some 2^-22 of the cap, whatever is left of a small tanh.)
-__device__ __forceinline__ float capped(float x, float cap) {
-    return __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x)), cap);
-}
+// With x = c s:  cap tanh(x / 2 log2(e)) = 2 cap y + cap, y = -1 / (1 + 2^x), as tanh(z) = 1 - 2 / (1 + e^(2 z)).  This is y; the rest goes into the
+// exponent that the softmax takes anyway.  An infinite exponential gives the cap, none its negative.  (Off by some 2^-21 of the cap beside exact
+// values, whatever is left of a small tanh.)
+__device__ __forceinline__ float tanh_part(float x) { return __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(x)); }
 
 // A row's maximum is raised, and what it has so far multiplied, only where a score is beyond it by more than this (in powers of two): weights
 // are then at most 2^8, which costs no bits, and most tiles raise nothing.
@@ -160,12 +160,25 @@ __device__ __forceinline__ Seen seen_from(const AttnItem &it, const AttnBounds &
 }
 
 // A row's bias: - slope |position - t|, slope times log2(e).
+//
+// In a tile that is a run of tokens, none of which a row sees before its position, that is slope (t0 - position) + slope k for the tile's first
+// token t0 and the number k of a key in it: the first part is added once, to what is taken off all of a lane's exponents, and the second is one operation with a
+// constant a score.  Tiles in which first tokens end, or of a prefix beyond a row's position, take each distance.  (Tails of 256 to 1024 tokens over 8 to
+// 32 K keys, us: each distance LATER, so LATER, without a bias LATER.)
 struct Bias {
     float slope;
     uint32_t position;
 };
 __device__ __forceinline__ Bias bias_of(const ScoredArgs &a, const AttnItem &it, uint32_t head, uint32_t row) {
     return {a.slopes ? 1.4426950408889634f * a.slopes[head * a.group + row % a.group] : 0.f, it.hit + row / a.group};
+}
+// Whether the bias is a line over places [v0, v0 + n), of rows from the one at `position` on.
+__device__ __forceinline__ bool is_line(const AttnItem &it, const RowsSee &r, uint32_t v0, uint32_t n, uint32_t position) {
+    const uint32_t last = v0 + n - 1 < it.sinks ? v0 + n - 1 : v0 + n - 1 + it.gap;
+    return (v0 >= it.sinks || v0 + n <= it.sinks || it.gap == 0) && (r.hi0 == position + 1 || last <= position);
+}
+__device__ __forceinline__ float line_begin(const AttnItem &it, const Bias &b, uint32_t place) {
+    return b.slope * (float)(int)((place < it.sinks ? place : place + it.gap) - b.position);
 }
 __device__ __forceinline__ float distance(const AttnItem &it, uint32_t place, uint32_t position) {
     const int d = (int)(position - (place < it.sinks ? place : place + it.gap));
@@ -275,7 +288,7 @@ __device__ __forceinline__ void write_lse(const AttnArgs &a, uint32_t token0, ui
 // the next keys: there HALVES = 2, and two wavefronts take the same tile of keys, half of the rows each; what the second one loads is in the caches.
 // (32 requests of 21 to 42 rows, 8-bit heads of 128: 59 us with three tiles of rows a wavefront and five such loads for each of keys, 51 so.)
 template <typename T, bool E4M3, int D, int RT, int HALVES, bool SCORED = false>
-__global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const ArgsOf<SCORED> a) {
+__global__ void __launch_bounds__(256, SCORED && E4M3 && RT == 1 ? 3 : 2) kvl_attn_few_kernel(const ArgsOf<SCORED> a) {
     constexpr int KT = few_rows_tile(D), NB = KT / 16;        // keys of a tile, blocks of 16
     constexpr int RB = D * (E4M3 ? 1 : 2);                          // bytes of a row
     constexpr int PR = RB / 16;                                     // pieces of 16 bytes in it
@@ -346,6 +359,7 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const ArgsOf<SCORE
     }
     x8 q[kStaged ? 1 : CH];
     const RowsSee see = rows_see<SCORED>(a, it, it.first_row, it.first_row + it.n_rows - 1);
+    const uint32_t p0 = it.hit + it.first_row / a.group;
 #pragma unroll
     for (int r = 0; r < kTiles; ++r) {
         const uint32_t i = min(r * 16 + n, it.n_rows - 1), row = it.first_row + i, token = row / a.group;
@@ -443,17 +457,27 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const ArgsOf<SCORE
                         const float x = s[r][b][i];
                         s[r][b][i] = E4M3 ? __builtin_fmaf(x, kc[i], kl[i]) : x * kc[i];
                         if constexpr (SCORED) {
-                            if (a.cap != 0.f) s[r][b][i] = capped(x * kc[i], a.cap) + (E4M3 ? kl[i] : 0.f);
+                            if (a.cap != 0.f) s[r][b][i] = __builtin_fmaf(2.f * a.cap, tanh_part(x * kc[i]), kl[i]);
                         }
                     }
                 }
+                float more = 0.f;                   // of a lane's scores
                 if constexpr (SCORED) {
+                    more = a.cap;
                     if (a.slopes) {
                         const Bias bias = kStaged ? biases[((R0 + r) * HALVES + half) * 16 + n] : bias_here;
+                        if (is_line(it, see, v0, KT, p0)) {
+                            more += line_begin(it, bias, v0) + bias.slope * (float)(4 * g);
 #pragma unroll
-                        for (int b = 0; b < NB; ++b)
+                            for (int b = 0; b < NB; ++b)
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) s[r][b][i] -= bias.slope * distance(it, v0 + 16 * b + 4 * g + i, bias.position);
+                                for (int i = 0; i < 4; ++i) s[r][b][i] = __builtin_fmaf(bias.slope, (float)(16 * b + i), s[r][b][i]);
+                        } else {
+#pragma unroll
+                            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) s[r][b][i] -= bias.slope * distance(it, v0 + 16 * b + 4 * g + i, bias.position);
+                        }
                     }
                 }
                 if (!whole) {
@@ -468,7 +492,7 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const ArgsOf<SCORE
                 for (int b = 0; b < NB; ++b)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) top = fmaxf(top, s[r][b][i]);
-                top = max_quarters(top);
+                top = max_quarters(SCORED ? top + more : top);
                 if (__any(top > m[R0 + r] + kSlack)) {
                     const float to = fmaxf(m[R0 + r], top), f = factor(m[R0 + r], to);
                     m[R0 + r] = to;
@@ -476,7 +500,7 @@ __global__ void __launch_bounds__(256, 2) kvl_attn_few_kernel(const ArgsOf<SCORE
 #pragma unroll
                     for (int d = 0; d < DC; ++d) o[R0 + r][d] *= f;
                 }
-                const float from = m[R0 + r] == -__builtin_inff() ? 0.f : m[R0 + r] - kLift<T>;
+                const float from = m[R0 + r] == -__builtin_inff() ? 0.f : m[R0 + r] - kLift<T> - (SCORED ? more : 0.f);
 #pragma unroll
                 for (int b = 0; b < NB; b += 2) {
                     u32x4 w, rest;
@@ -662,6 +686,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
     const RowsSee all_see = rows_see<SCORED>(a, it, it.first_row, it.first_row + it.n_rows - 1);
     const RowsSee see = rows_see<SCORED>(a, it, it.first_row + min(rows_before, it.n_rows - 1), it.first_row + min(rows_before + 31, it.n_rows - 1));
     const Seen seen = seen_from(it, bounds_of<SCORED>(a, it, row));
+    const uint32_t w0 = it.hit + (it.first_row + min(rows_before, it.n_rows - 1)) / a.group;
     Bias bias{};
     if constexpr (SCORED) bias = bias_of(a, it, head, row);
     x8 q[CH];
@@ -778,22 +803,31 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[b][i] *= of_key(by.k, 32 * b + 8 * (i / 4) + i % 4);
         }
-        float c = a.c;
-        if constexpr (SCORED) {                     // (scores that are made anew are in powers of two from there on)
+        float c = a.c, more = 0.f;                  // a score, in powers of two, is c s + more
+        if constexpr (SCORED) {
             if (a.cap != 0.f) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[b][i] = capped(s[b][i] * c, a.cap);
-                c = 1.f;
+                    for (int i = 0; i < 16; ++i) s[b][i] = tanh_part(s[b][i] * c);
+                c = 2.f * a.cap;
+                more = a.cap;
             }
             if (a.slopes) {
+                const float slope = bias.slope * a.over;
+                if (is_line(it, see, v0, KT, w0)) {
+                    more += line_begin(it, bias, v0) + bias.slope * (float)(4 * h);
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+                    for (int b = 0; b < 2; ++b)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        s[b][i] = __builtin_fmaf(s[b][i], c, -bias.slope * distance(it, v0 + 4 * h + 32 * b + 8 * (i / 4) + i % 4, bias.position));
-                c = 1.f;
+                        for (int i = 0; i < 16; ++i) s[b][i] = __builtin_fmaf(slope, (float)(32 * b + 8 * (i / 4) + i % 4), s[b][i]);
+                } else {
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            s[b][i] -= slope * distance(it, v0 + 4 * h + 32 * b + 8 * (i / 4) + i % 4, bias.position);
+                }
             }
         }
         if (!whole) {
@@ -809,7 +843,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-        top = max_halves(top) * c;
+        top = SCORED ? max_halves(__builtin_fmaf(top, c, more)) : max_halves(top) * c;
         if (__any(top > m + kSlack)) {
             const float to = fmaxf(m, top), f = factor(m, to);
             m = to;
@@ -819,7 +853,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] *= f;
         }
-        const float from = m == -__builtin_inff() ? 0.f : kLift<T> - m;
+        const float from = m == -__builtin_inff() ? 0.f : kLift<T> - m + (SCORED ? more : 0.f);
         // the weights of keys 16 u + 8 (i / 4) + 4 h + i % 4 and the next, i even
         auto weights = [&](int u, int i) {
             const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u / 2][8 * (u % 2) + i], c, from));
