@@ -16,7 +16,8 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libkvl.so")
 # for this interpreter alone: the module is laid out by its headers
 NATIVE = os.path.join(_HERE, "_native" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
-NATIVE_SOURCES = [os.path.join(_ROOT, "include", "kvl.h"), os.path.join(_ROOT, "include", "kvl_attn.h"), os.path.join(CSRC, "kvl_python.cpp")]
+NATIVE_SOURCES = [os.path.join(_ROOT, "include", "kvl.h"), os.path.join(_ROOT, "include", "kvl_attn.h"),
+                  os.path.join(_ROOT, "include", "kvl_pages.h"), os.path.join(CSRC, "kvl_python.cpp")]
 SOURCES = ["kvl_plan.hip", "kvl_kernels.hip", "kvl_h2d.hip", "kvl_stream.hip", "kvl_noalloc.hip", "kvl_attn_plan.hip",
            "kvl_append.hip", "kvl_attn.hip", "kvl_attn_join.hip", "kvl_copy_blocks.hip", "kvl_pages.cpp", "kvl_sched.cpp"]
 

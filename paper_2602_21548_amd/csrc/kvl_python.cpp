@@ -13,6 +13,7 @@
 #include <cstdint>
 
 #include "kvl_attn.h"
+#include "kvl_pages.h"
 
 namespace {
 
@@ -50,6 +51,11 @@ struct Library {
     decltype(&kvl_attn_layer) attn;
     decltype(&kvl_attn_scored_layer) scored;
     decltype(&kvl_attn_join) join;
+    decltype(&kvl_pages_fork) fork;
+    decltype(&kvl_pages_extend) extend;
+    decltype(&kvl_pages_free) end;
+    decltype(&kvl_pages_tables) tables;
+    decltype(&kvl_copy_blocks) copy_blocks;
 } g_lib;
 PyObject *g_float32;
 PyObject *g_tensor_type, *g_array_type, *g_raw_stream, *g_get_device, *g_is_initialized;
@@ -431,6 +437,82 @@ PyObject *requests(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return PyBool_FromLong(ok);
 }
 
+// The pages' calls, for arrays that pages.py has made or looked at: contiguous ones of numbers of the size named here.  They return what the library
+// returned; a buffer that is not what it should be is a TypeError.
+struct Array {
+    Py_buffer view;
+    bool held = false;
+    ~Array() {
+        if (held) PyBuffer_Release(&view);
+    }
+    bool get(PyObject *o, Py_ssize_t item, bool write) {
+        if (PyObject_GetBuffer(o, &view, write ? PyBUF_CONTIG : PyBUF_CONTIG_RO) != 0) return false;
+        held = true;
+        if (view.itemsize == item) return true;
+        PyErr_SetString(PyExc_TypeError, "an array of other numbers");
+        return false;
+    }
+    uint64_t size() const { return (uint64_t)(view.len / view.itemsize); }
+    template <typename T>
+    T *as() const { return (T *)view.buf; }
+};
+void *handle_of(PyObject *o) { return PyLong_AsVoidPtr(o); }     // (0 where it is no number: the library refuses it)
+#define KVL_ARRAY(name, at, type, write)                                                                                 Array name;                                                                                                          if (!name.get(a[at], sizeof(type), write)) return nullptr
+#define KVL_PAGES(count)                                                                                                 if (n != count) {                                                                                                        PyErr_SetString(PyExc_TypeError, "wrong number of arguments");                                                       return nullptr;                                                                                                  }                                                                                                                    void *pages = handle_of(a[0]);                                                                                       if (PyErr_Occurred()) return nullptr
+
+PyObject *pages_fork(PyObject *, PyObject *const *a, Py_ssize_t n) {        // handle, sequences, numbers of the forks
+    KVL_PAGES(3);
+    KVL_ARRAY(from, 1, uint64_t, false);
+    KVL_ARRAY(to, 2, uint64_t, true);
+    if (to.size() < from.size()) return PyLong_FromLong(KVL_EINVAL);
+    return PyLong_FromLong(g_lib.fork((kvl_pages_t *)pages, from.as<uint64_t>(), (uint32_t)from.size(), to.as<uint64_t>()));
+}
+// handle, sequences, tokens, copies; what is not negative is how many copies there are
+PyObject *pages_extend(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    KVL_PAGES(4);
+    KVL_ARRAY(sequences, 1, uint64_t, false);
+    KVL_ARRAY(tokens, 2, uint32_t, false);
+    KVL_ARRAY(copies, 3, int32_t, true);
+    if (tokens.size() != sequences.size() || copies.size() < 2 * sequences.size()) return PyLong_FromLong(KVL_EINVAL);
+    uint32_t made = 0;
+    const int rc = g_lib.extend((kvl_pages_t *)pages, sequences.as<uint64_t>(), tokens.as<uint32_t>(), (uint32_t)sequences.size(),
+                                copies.as<kvl_block_copy_t>(), &made);
+    return PyLong_FromLong(rc != KVL_OK ? rc : (long)made);
+}
+PyObject *pages_free(PyObject *, PyObject *const *a, Py_ssize_t n) {        // handle, sequences
+    KVL_PAGES(2);
+    KVL_ARRAY(sequences, 1, uint64_t, false);
+    return PyLong_FromLong(g_lib.end((kvl_pages_t *)pages, sequences.as<uint64_t>(), (uint32_t)sequences.size()));
+}
+PyObject *pages_tables(PyObject *, PyObject *const *a, Py_ssize_t n) {      // handle, sequences, table, first
+    KVL_PAGES(4);
+    KVL_ARRAY(sequences, 1, uint64_t, false);
+    KVL_ARRAY(table, 2, int32_t, true);
+    KVL_ARRAY(first, 3, uint64_t, true);
+    if (first.size() <= sequences.size()) return PyLong_FromLong(KVL_EINVAL);
+    return PyLong_FromLong(g_lib.tables((const kvl_pages_t *)pages, sequences.as<uint64_t>(), (uint32_t)sequences.size(), table.as<int32_t>(),
+                                        table.size(), first.as<uint64_t>()));
+}
+PyObject *copy_blocks(PyObject *, PyObject *const *a, Py_ssize_t n) {       // handle, copies, stream
+    KVL_PAGES(3);
+    KVL_ARRAY(copies, 1, int32_t, false);
+    void *s;
+    if (!stream(a[2], &s)) KVL_NOT_TAKEN;
+    KVL_CALL(g_lib.copy_blocks((const kvl_page_pools_t *)pages, copies.as<kvl_block_copy_t>(), copies.size() / 2, s));
+}
+
+// setup_pages(the addresses of the pages' five entry points)
+PyObject *setup_pages(PyObject *, PyObject *args) {
+    unsigned long long f[5];
+    if (!PyArg_ParseTuple(args, "KKKKK", &f[0], &f[1], &f[2], &f[3], &f[4])) return nullptr;
+    g_lib.fork = (decltype(g_lib.fork))(uintptr_t)f[0];
+    g_lib.extend = (decltype(g_lib.extend))(uintptr_t)f[1];
+    g_lib.end = (decltype(g_lib.end))(uintptr_t)f[2];
+    g_lib.tables = (decltype(g_lib.tables))(uintptr_t)f[3];
+    g_lib.copy_blocks = (decltype(g_lib.copy_blocks))(uintptr_t)f[4];
+    Py_RETURN_NONE;
+}
+
 // setup(torch.Tensor, numpy.ndarray, torch's three stream functions, the addresses of the library's five entry points)
 PyObject *setup(PyObject *, PyObject *args) {
     PyObject *type, *array, *raw, *device, *initialized;
@@ -581,6 +663,12 @@ PyMethodDef module_methods[] = {
     {"requests", (PyCFunction)(void (*)(void))requests, METH_FASTCALL, nullptr},
     {"setup", setup, METH_VARARGS, nullptr},
     {"setup_attn", setup_attn, METH_VARARGS, nullptr},
+    {"pages_fork", (PyCFunction)(void (*)(void))pages_fork, METH_FASTCALL, nullptr},
+    {"pages_extend", (PyCFunction)(void (*)(void))pages_extend, METH_FASTCALL, nullptr},
+    {"pages_free", (PyCFunction)(void (*)(void))pages_free, METH_FASTCALL, nullptr},
+    {"pages_tables", (PyCFunction)(void (*)(void))pages_tables, METH_FASTCALL, nullptr},
+    {"copy_blocks", (PyCFunction)(void (*)(void))copy_blocks, METH_FASTCALL, nullptr},
+    {"setup_pages", setup_pages, METH_VARARGS, nullptr},
     {"forked", forked, METH_NOARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

@@ -47,16 +47,42 @@ for _name, (_res, _args) in SIGNATURES.items():
     _fn.restype, _fn.argtypes = _res, _args
 
 
+def _fork(pages: int, s: np.ndarray, out: np.ndarray) -> int:
+    return _lib.kvl_pages_fork(pages, s.ctypes.data, s.size, out.ctypes.data)
+
+
+def _extend(pages: int, s: np.ndarray, tokens: np.ndarray, copies: np.ndarray) -> int:
+    n = C.c_uint32()
+    return _lib.kvl_pages_extend(pages, s.ctypes.data, tokens.ctypes.data, s.size, copies.ctypes.data, C.byref(n)) or n.value
+
+
+def _free(pages: int, s: np.ndarray) -> int:
+    return _lib.kvl_pages_free(pages, s.ctypes.data, s.size)
+
+
+def _tables(pages: int, s: np.ndarray, table: np.ndarray, first: np.ndarray) -> int:
+    return _lib.kvl_pages_tables(pages, s.ctypes.data, s.size, table.ctypes.data if table.size else None, table.size, first.ctypes.data)
+
+
+_copy = _b._not_taken
+if _b._native is not None:
+    # (by ctypes a call takes some microseconds more)
+    _b._native.setup_pages(*(C.cast(getattr(_lib, f), C.c_void_p).value
+                             for f in ("kvl_pages_fork", "kvl_pages_extend", "kvl_pages_free", "kvl_pages_tables", "kvl_copy_blocks")))
+    _fork, _extend, _free, _tables = _b._native.pages_fork, _b._native.pages_extend, _b._native.pages_free, _b._native.pages_tables
+    _copy = _b._native.copy_blocks
+
+
 class _Owner:
     """Of a handle."""
 
     def __init__(self, handle: int, destroy):
-        self._h, self._destroy = C.c_void_p(handle), destroy
+        self._h, self._destroy = handle, destroy
 
     def destroy(self) -> None:
         if self._h:
             self._destroy(self._h)
-            self._h = C.c_void_p(None)
+            self._h = None
 
     def __del__(self):
         try:
@@ -72,7 +98,7 @@ class _Owner:
         return False
 
     @property
-    def handle(self) -> C.c_void_p:
+    def handle(self) -> int:
         if not self._h:
             raise ValueError("destroyed")
         return self._h
@@ -84,6 +110,7 @@ class Pages(_Owner):
     def __init__(self, handle: int, block_tokens: int, pool_blocks: int):
         super().__init__(handle, _lib.kvl_pages_destroy)
         self.block_tokens, self.pool_blocks = block_tokens, pool_blocks
+        self._longest = 64                      # entries of tables that were asked for
 
 
 class PagePools(_Owner):
@@ -114,8 +141,10 @@ def _sequences(x, what: str) -> np.ndarray:
 
 def _per_sequence(tokens, n: int, what: str) -> np.ndarray:
     """One number for all sequences, or one for each."""
+    if type(tokens) is int and 0 <= tokens < 1 << 32:
+        return np.full(n, tokens, dtype=np.uint32)
     if isinstance(tokens, (int, np.integer)):
-        tokens = np.full(n, _numbers([tokens], np.uint32, f"{what} tokens")[0])
+        tokens = [int(tokens)] * n
     tokens = _numbers(tokens, np.uint32, f"{what} tokens")
     if tokens.size != n:
         raise ValueError(f"{what}: need tokens for every sequence")
@@ -144,8 +173,8 @@ def kvl_pages_adopt(pages: Pages, tables: Sequence[np.ndarray], tokens) -> np.nd
 def kvl_pages_fork(pages: Pages, sequences) -> np.ndarray:
     """New sequences that are what these are now; their numbers."""
     s = _sequences(sequences, "kvl_pages_fork")
-    out = np.zeros(s.size, dtype=np.uint64)
-    _b._check(_lib.kvl_pages_fork(pages.handle, s.ctypes.data, s.size, out.ctypes.data), "kvl_pages_fork")
+    out = np.empty(s.size, dtype=np.uint64)
+    _b._check(_fork(pages.handle, s, out), "kvl_pages_fork")
     return out
 
 
@@ -154,9 +183,11 @@ def kvl_pages_extend(pages: Pages, sequences, tokens) -> np.ndarray:
     int32 [copies, 2], from and to."""
     s = _sequences(sequences, "kvl_pages_extend")
     t = _per_sequence(tokens, s.size, "kvl_pages_extend")
-    copies, n = np.empty((s.size, 2), dtype=np.int32), C.c_uint32()
-    _b._check(_lib.kvl_pages_extend(pages.handle, s.ctypes.data, t.ctypes.data, s.size, copies.ctypes.data, C.byref(n)), "kvl_pages_extend")
-    return copies[:n.value]
+    copies = np.empty((s.size, 2), dtype=np.int32)
+    n = _extend(pages.handle, s, t, copies)
+    if n < 0:
+        _b._check(n, "kvl_pages_extend")
+    return copies[:n]
 
 
 def kvl_pages_truncate(pages: Pages, sequences, tokens) -> None:
@@ -169,7 +200,7 @@ def kvl_pages_truncate(pages: Pages, sequences, tokens) -> None:
 def kvl_pages_free(pages: Pages, sequences) -> None:
     """Sequences end."""
     s = _sequences(sequences, "kvl_pages_free")
-    _b._check(_lib.kvl_pages_free(pages.handle, s.ctypes.data, s.size), "kvl_pages_free")
+    _b._check(_free(pages.handle, s), "kvl_pages_free")
 
 
 def kvl_pages_compact(pages: Pages, most: int = None) -> np.ndarray:
@@ -188,15 +219,15 @@ def kvl_pages_compact(pages: Pages, most: int = None) -> np.ndarray:
 def kvl_pages_tables(pages: Pages, sequences) -> List[np.ndarray]:
     """The block table of each sequence (int32; parts of one array)."""
     s = _sequences(sequences, "kvl_pages_tables")
-    first = np.zeros(s.size + 1, dtype=np.uint64)
-    rc = _lib.kvl_pages_tables(pages.handle, s.ctypes.data, s.size, None, 0, first.ctypes.data)
-    if rc != _b.KVL_ESPACE:
-        _b._check(rc, "kvl_pages_tables")
-    table = np.empty(int(first[-1]), dtype=np.int32)
-    if table.size:
-        _b._check(_lib.kvl_pages_tables(pages.handle, s.ctypes.data, s.size, table.ctypes.data, table.size, first.ctypes.data), "kvl_pages_tables")
+    first, table = np.empty(s.size + 1, dtype=np.uint64), np.empty(pages._longest, dtype=np.int32)
+    rc = _tables(pages.handle, s, table, first)
+    if rc == _b.KVL_ESPACE:
+        table = np.empty(int(first[-1]), dtype=np.int32)
+        pages._longest = table.size
+        rc = _tables(pages.handle, s, table, first)
+    _b._check(rc, "kvl_pages_tables")
     at = first.tolist()
-    return [table[a:b] for a, b in zip(at[:-1], at[1:])]
+    return [table[a:b] for a, b in zip(at, at[1:])]
 
 
 def kvl_pages_tokens(pages: Pages, sequences) -> np.ndarray:
@@ -243,4 +274,7 @@ def kvl_copy_blocks(pools: PagePools, copies, stream=None) -> None:
         if c.ndim != 2 or c.shape[1] != 2 or (c.size and (c.dtype.kind not in "iu" or abs(c.astype(np.int64)).max() >= 1 << 31)):
             raise ValueError("kvl_copy_blocks: copies must be whole numbers [copies, 2]")
         c = np.ascontiguousarray(c, dtype=np.int32)
-    _b._check(_lib.kvl_copy_blocks(pools.handle, c.ctypes.data, c.shape[0], _b._stream_handle(stream)), "kvl_copy_blocks")
+    rc = _copy(pools.handle, c, stream)
+    if rc > 0:
+        rc = _lib.kvl_copy_blocks(pools.handle, c.ctypes.data, c.shape[0], _b._stream_handle(stream))
+    _b._check(rc, "kvl_copy_blocks")
