@@ -1,6 +1,7 @@
 // Results of attention over different keys, joined.
 #include "kvl_attn_internal.h"
 #include "kvl_attn_types.h"
+#include "kvl_vectors.h"
 
 namespace kvl {
 
@@ -17,10 +18,15 @@ struct JoinParts {
 // With w_i = 2^(log2(e) (lse_i - m)), m the largest lse:  out = sum_i w_i x_i / sum_i w_i,  lse = m + log(sum_i w_i).
 //
 // The bytes bound it: a lane has 8 elements of all parts (at most N) on their way at once, and its row's lses, which the D / 8 lanes of the row
-// read together.
-template <typename T, int D, int N>
-__global__ void __launch_bounds__(256) kvl_attn_join_parts_kernel(const JoinParts a) {
-    const uint64_t first = (uint64_t)blockIdx.x * 256, token0 = first / a.per_token;
+// read together.  PAST: loads and stores pass by the caches, in workgroups of half the size, which suits what is more than these hold (four parts of 64
+// heads of 128, us, with the caches / past them: 83 MB 13.9 / 16.2, 166 MB 32.3 / 30.2, 333 MB 62.5 / 56.8, 666 MB, 6.1 TB/s, 122.9 / 108.6).
+constexpr uint64_t kJoinPastBytes = 128u << 20;
+template <bool PAST>
+constexpr uint32_t kJoinThreads = PAST ? 128 : 256;
+
+template <typename T, int D, int N, bool PAST>
+__global__ void __launch_bounds__(kJoinThreads<PAST>) kvl_attn_join_parts_kernel(const JoinParts a) {
+    const uint64_t first = (uint64_t)blockIdx.x * kJoinThreads<PAST>, token0 = first / a.per_token;
     if (first + threadIdx.x >= a.pieces) return;
     const uint32_t at = (uint32_t)(first - token0 * a.per_token) + threadIdx.x, beyond = at / a.per_token, piece = at - beyond * a.per_token;
     const uint64_t token = token0 + beyond, row = token * a.heads + piece / (D / 8);
@@ -32,7 +38,7 @@ __global__ void __launch_bounds__(256) kvl_attn_join_parts_kernel(const JoinPart
         x[i] = u32x4{0, 0, 0, 0};
         if ((uint32_t)i < a.n) {
             w[i] = a.lses[i][row];
-            x[i] = *reinterpret_cast<const u32x4 *>(a.parts[i] + 2 * (token * a.strides[i] + piece * 8));
+            x[i] = load16<PAST>((gsrc_t)(uintptr_t)(a.parts[i] + 2 * (token * a.strides[i] + piece * 8)));
         }
     }
     float top = w[0];
@@ -56,16 +62,23 @@ __global__ void __launch_bounds__(256) kvl_attn_join_parts_kernel(const JoinPart
     u32x4 y;
 #pragma unroll
     for (int j = 0; j < 4; ++j) y[j] = narrow<T>(e[2 * j] * over, e[2 * j + 1] * over);
-    *reinterpret_cast<u32x4 *>(a.out + 2 * (token * a.out_stride + piece * 8)) = y;
+    store16<PAST ? 1 : 0>((gdst_t)(uintptr_t)(a.out + 2 * (token * a.out_stride + piece * 8)), y);
     // (the lanes of a row are in one wavefront: all have read its lses)
     if (a.lse && piece % (D / 8) == 0) a.lse[row] = top + 0.69314718055994531f * __log2f(sum);
 }
 
+template <typename T, int D, bool PAST>
+static void launch_parts(const JoinParts &a, hipStream_t stream) {
+    constexpr uint32_t kThreads = kJoinThreads<PAST>;
+    const uint32_t groups = (uint32_t)((a.pieces + kThreads - 1) / kThreads);
+    if (a.n <= 2) kvl_attn_join_parts_kernel<T, D, 2, PAST><<<groups, kThreads, 0, stream>>>(a);
+    else if (a.n <= 4) kvl_attn_join_parts_kernel<T, D, 4, PAST><<<groups, kThreads, 0, stream>>>(a);
+    else kvl_attn_join_parts_kernel<T, D, (int)KVL_JOIN_MOST, PAST><<<groups, kThreads, 0, stream>>>(a);
+}
 template <typename T, int D>
-static void launch_join(const JoinParts &a, uint32_t groups, hipStream_t stream) {
-    if (a.n <= 2) kvl_attn_join_parts_kernel<T, D, 2><<<groups, 256, 0, stream>>>(a);
-    else if (a.n <= 4) kvl_attn_join_parts_kernel<T, D, 4><<<groups, 256, 0, stream>>>(a);
-    else kvl_attn_join_parts_kernel<T, D, (int)KVL_JOIN_MOST><<<groups, 256, 0, stream>>>(a);
+static void launch_join(const JoinParts &a, hipStream_t stream) {
+    if ((a.n + 1) * a.pieces * 16 > kJoinPastBytes) launch_parts<T, D, true>(a, stream);
+    else launch_parts<T, D, false>(a, stream);
 }
 
 static int attn_join(const kvl_attn_plan_t *plan, const kvl_attn_join_t *in, hipStream_t stream) {
@@ -82,8 +95,7 @@ static int attn_join(const kvl_attn_plan_t *plan, const kvl_attn_join_t *in, hip
     a.per_token = (uint32_t)(row / 8);
     a.pieces = n * a.per_token;
     a.out_stride = in->out_stride;
-    const uint64_t groups = (a.pieces + 255) / 256;
-    if (groups >= (1u << 24)) return KVL_ERANGE;            // fewer than 2^32 lanes
+    if (a.pieces > UINT32_MAX - 256) return KVL_ERANGE;      // (a lane each, in whole workgroups)
     auto lse_row = [&](const float *lse) {
         uint64_t dense = 0;
         return reinterpret_cast<uintptr_t>(lse) % 4 ? (int)KVL_EINVAL : check_rows(plan, lse, n, l.q_heads, &dense, false);
@@ -101,8 +113,8 @@ static int attn_join(const kvl_attn_plan_t *plan, const kvl_attn_join_t *in, hip
     }
     a.out = static_cast<char *>(in->out);
     a.lse = in->lse;
-    if (l.dtype == KVL_F16) l.head_dim == 128 ? launch_join<F16, 128>(a, (uint32_t)groups, stream) : launch_join<F16, 64>(a, (uint32_t)groups, stream);
-    else l.head_dim == 128 ? launch_join<Bf16, 128>(a, (uint32_t)groups, stream) : launch_join<Bf16, 64>(a, (uint32_t)groups, stream);
+    if (l.dtype == KVL_F16) l.head_dim == 128 ? launch_join<F16, 128>(a, stream) : launch_join<F16, 64>(a, stream);
+    else l.head_dim == 128 ? launch_join<Bf16, 128>(a, stream) : launch_join<Bf16, 64>(a, stream);
     KVL_HIP(hipGetLastError());
     return KVL_OK;
 }

@@ -298,6 +298,23 @@ def test_join(n, tokens, heads, dim, dtype):
     assert torch.equal(out, again)
 
 
+def test_a_large_join():
+    """More than the caches hold: 3 parts of 700 tokens of 128 heads, of which the rows of some tokens are looked at."""
+    n, h, d, dtype = 700, 128, 128, torch.bfloat16
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    parts = [torch.randn(n, h, d, device="cuda", generator=g).to(dtype) for _ in range(5)]
+    lses = [torch.randn(n, h, device="cuda", generator=g) for _ in range(5)]
+    assert 6 * n * h * d * 2 > 128 << 20
+    out, lse = torch.full((n, h, d), NAN, dtype=dtype, device="cuda"), torch.full((n, h), NAN, device="cuda")
+    K.kvl_attn_join(join_plan(n, h, d, dtype), parts, lses, out, lse)
+    at = [0, 1, 255, 256, 699]
+    joined_right([x[at].cpu() for x in parts], [l[at].cpu() for l in lses], out[at], lse[at], dtype)
+    w = torch.softmax(torch.stack(lses).double(), 0)
+    near = sum(x.double() * y[..., None] for x, y in zip(parts, w))
+    assert float((out.double() - near).abs().max()) < 2.0 ** -8 * float(near.abs().max()) + 2.0 ** -18
+
+
 def test_join_in_place_and_at_strides():
     p = join_plan(40, 6, 64, torch.bfloat16)
     parts, lses = some_parts(3, 40, 6, 64, torch.bfloat16)

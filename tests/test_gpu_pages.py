@@ -43,11 +43,26 @@ def test_planes_that_begin_anywhere(size, shift):
     check(2, 6, [size, 64], [[1, 0], [4, 5]], shift=shift)
 
 
-@pytest.mark.parametrize("n", [0, 1, 23, 24, 25, 447, 448, 449, 1000])
+@pytest.mark.parametrize("n", [0, 1, 23, 24, 25, 319, 320, 321, 1000])
 def test_numbers_of_copies(n):
     """Around what one launch takes."""
     order = np.random.default_rng(n).permutation(2100)
     check(2, 2100, [144, 4], np.stack([order[:n], order[1000:1000 + n]], 1).astype(np.int32))
+
+
+@pytest.mark.parametrize("sizes,layers", [([65536, 65536, 32, 32], 2), ([1040], 1), ([9 << 20, 12, 5], 1)])
+def test_one_block_to_many(sizes, layers):
+    """More and fewer than share a workgroup, in lists that one launch does not take, of little and of much."""
+    order = np.random.default_rng(4).permutation(500)
+    blocks = 500 if max(sizes) < 1 << 20 else 40
+    order = order[order < blocks] if blocks < 500 else order
+    ways = [1, 8, 9, 7, 2] if blocks < 500 else [200, 1, 1, 7, 8, 9, 17, 40, 2]
+    frm = np.repeat(order[:len(ways)], ways)
+    check(layers, blocks, sizes, np.stack([frm, order[len(ways):len(ways) + len(frm)]], 1).astype(np.int32))
+
+
+def test_more_than_the_caches_hold():
+    check(3, 300, [1 << 20], np.stack([np.repeat(np.arange(50), 2), np.arange(100, 200)], 1).astype(np.int32))
 
 
 def test_one_block_to_many_and_lists_of_numbers():
