@@ -99,6 +99,7 @@ static int attn_layer(const kvl_attn_plan_t *plan, const kvl_attn_t *in, const k
     a.window = l.window && l.window < (1u << 31) ? l.window : 1u << 31;
     a.sinks = l.sinks;
     a.c = t.scale * 1.4426950408889634f;
+    a.near = (uint64_t)l.pool_blocks * l.block_tokens * l.kv_heads * l.head_dim * (codes ? 1 : 2) < 1ull << 32;
     if (how.cap != 0) {
         // (of a cap so small that no float holds the factor: the tanh is 1 of anything but 0)
         a.c = std::fmin(2 * a.c / how.cap, 0x1p126f);

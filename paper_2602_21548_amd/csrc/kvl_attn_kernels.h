@@ -37,6 +37,7 @@ struct AttnArgs {
     uint32_t kv_heads, group;
     uint32_t window, sinks;             // window: 2^31 where there is none
     float c;                            // scale * log2(e)
+    uint32_t near;                      // a plane has fewer than 2^32 bytes
 };
 
 // What the SCORED kernels take beside that; c is 2 log2(e) scale / cap where there is a cap.
@@ -147,6 +148,19 @@ __device__ __forceinline__ bool none_seen(const AttnItem &it, const RowsSee &r, 
     return t0 >= r.hi1 || (t1 < r.lo0 && t0 >= r.first);
 }
 
+// The same of tiles of n places, beyond the first tokens: most tiles are between the places from which and up to which that is so.
+struct Whole {
+    const AttnItem &it;
+    const RowsSee &rows;
+    uint32_t n, first, count;
+    __device__ __forceinline__ Whole(const AttnItem &item, const RowsSee &r, uint32_t tile) : it(item), rows(r), n(tile) {
+        first = max(it.sinks, max(r.lo1, it.gap) - it.gap);
+        const uint32_t end = min(it.end, max(r.hi0, it.gap) - it.gap);
+        count = end >= first + n ? end - n - first + 1 : 0;
+    }
+    __device__ __forceinline__ bool operator()(uint32_t v0) const { return v0 - first < count || all_seen(it, rows, v0, v0 + n - 1); }
+};
+
 // The places that a query sees among those before `end`: v - first < count, and v < sinks.  (The first place whose token is t or a later
 // one: t up to the first tokens' end, and t - gap beyond the gap.)
 struct Seen {
@@ -162,9 +176,10 @@ __device__ __forceinline__ Seen seen_from(const AttnItem &it, const AttnBounds &
 // A row's bias: - slope |position - t|, slope times log2(e).
 //
 // In a tile that is a run of tokens, none of which a row sees before its position, that is slope (t0 - position) + slope k for the tile's first
-// token t0 and the number k of a key in it: the first part is added once, to what is taken off all of a lane's exponents, and the second is one operation with a
-// constant a score.  Tiles in which first tokens end, or of a prefix beyond a row's position, take each distance.  (Tails of 256 to 1024 tokens over 8 to
-// 32 K keys, us: each distance LATER, so LATER, without a bias LATER.)
+// token t0 and the number k of a key in it.  The first part is added once, to what is taken off all of a lane's exponents.  The second is a product of keys by
+// rows, which the matrix unit adds: k is a bf16 number, the slope three of them (24 bits; products and sums are in 32 bits as the scores' are).  Tiles in
+// which first tokens end, or of a prefix beyond a row's position, take each distance.  (Tails of 256 to 1024 tokens over 8 to 32 K keys, us: each distance
+// 1435, one operation with a constant a score 1198, the matrix unit 1179, without a bias 1020.)
 struct Bias {
     float slope;
     uint32_t position;
@@ -177,8 +192,26 @@ __device__ __forceinline__ bool is_line(const AttnItem &it, const RowsSee &r, ui
     const uint32_t last = v0 + n - 1 < it.sinks ? v0 + n - 1 : v0 + n - 1 + it.gap;
     return (v0 >= it.sinks || v0 + n <= it.sinks || it.gap == 0) && (r.hi0 == position + 1 || last <= position);
 }
+// A bias that falls with distance makes later keys' scores the greater ones: tiles are taken from the last to the first, so that few raise a row's maximum (the
+// tails above from the first to the last: 1280 us).  The kernel for few rows waits for memory, whichever way it goes.
+template <bool SCORED>
+__device__ __forceinline__ uint32_t in_order(const ArgsOf<SCORED> &a, uint32_t tile, uint32_t tiles) {
+    if constexpr (SCORED) {
+        if (a.slopes) return tiles - 1 - min(tile, tiles - 1);
+    }
+    return tile;
+}
 __device__ __forceinline__ float line_begin(const AttnItem &it, const Bias &b, uint32_t place) {
     return b.slope * (float)(int)((place < it.sinks ? place : place + it.gap) - b.position);
+}
+// The operands of slope k: of the lane that names a row, and of the one that names key `key` of its tile.
+__device__ __forceinline__ u32x2 slope_parts(float slope, bool first) {
+    const float a = Bf16::widen(narrow<Bf16>(slope, 0.f))[0], b = Bf16::widen(narrow<Bf16>(slope - a, 0.f))[0];
+    return first ? u32x2{narrow<Bf16>(a, b), narrow<Bf16>(slope - a - b, 0.f)} : u32x2{0, 0};
+}
+__device__ __forceinline__ u32x2 key_parts(uint32_t key, bool first) {
+    const uint32_t w = narrow<Bf16>((float)key, (float)key);
+    return first ? u32x2{w, w & 0xffffu} : u32x2{0, 0};
 }
 __device__ __forceinline__ float distance(const AttnItem &it, uint32_t place, uint32_t position) {
     const int d = (int)(position - (place < it.sinks ? place : place + it.gap));
@@ -467,11 +500,10 @@ __global__ void __launch_bounds__(256, SCORED && E4M3 && RT == 1 ? 3 : 2) kvl_at
                     if (a.slopes) {
                         const Bias bias = kStaged ? biases[((R0 + r) * HALVES + half) * 16 + n] : bias_here;
                         if (is_line(it, see, v0, KT, p0)) {
-                            more += line_begin(it, bias, v0) + bias.slope * (float)(4 * g);
+                            more += line_begin(it, bias, v0);
+                            const u32x2 slope = slope_parts(bias.slope, g == 0);
 #pragma unroll
-                            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) s[r][b][i] = __builtin_fmaf(bias.slope, (float)(16 * b + i), s[r][b][i]);
+                            for (int b = 0; b < NB; ++b) s[r][b] = Bf16::add16(key_parts(16 * b + n, g == 0), slope, s[r][b]);
                         } else {
 #pragma unroll
                             for (int b = 0; b < NB; ++b)
@@ -627,9 +659,10 @@ __global__ void __launch_bounds__(256, SCORED && E4M3 && RT == 1 ? 3 : 2) kvl_at
 // its codes alone there, keys' as fp16, values' as bf16; the keys' scales multiply scores, the values' the weights, in 32 bits, and a weight is two
 // bf16 numbers, the second one what the first leaves (their products with codes are exact, and a weight keeps 16 bits).
 //
-// The matrix instructions (37 % of the time busy) and the vector unit (46 %, most of it the exponentials and what goes with them) bound it, which
-// the two wavefronts that a SIMD has registers for do not overlap well: 810 to 850 TFLOP/s (by the card) in 8-bit tails over long prefixes, heads of 128; of 64,
-// 26 % and 55 %, 610 to 630 under a window.
+// What bounds it is how many instructions two wavefronts a SIMD issue for a tile (the matrix unit is busy for 36 to 40 % of the time, the vector unit for 30 to 46 %, and
+// each instruction taken out of a tile's loop takes its share of the time with it): so a tile's keys and values are addressed from one register each,
+// in the LDS (rows padded, not turned: 1020 to 970 us for 16-bit tails over 8 to 32 K keys, with the next two) and in memory (32 bits from one address), and what all rows see is
+// two numbers.  870 TFLOP/s there, 950 over an 8-bit cache (by the card; the library's product of 8192^3 reaches 1207); heads of 64, 600 under a window.
 template <typename T, bool E4M3>
 __device__ __forceinline__ void codes_to_half(u32x4 w, float scale, u32x4 *x, u32x4 *y) {
     uint32_t e[8];
@@ -654,6 +687,26 @@ __device__ __forceinline__ void codes_to_half(u32x4 w, float scale, u32x4 *x, u3
 // Scales that leave codes in fp16's range.
 __device__ __forceinline__ bool suits_f16(float scale) { return scale >= 0x1p-15f && scale <= 0x1p7f; }
 
+// The order in which the compiler puts instructions: groups of N of a kind, one after the other.
+constexpr int kMatrix = 0x8, kLdsReads = 0x100;
+template <int KIND, int N>
+__device__ __forceinline__ void in_turn() {
+    __builtin_amdgcn_sched_group_barrier(KIND, N, 0);
+}
+template <int N, typename F>
+__device__ __forceinline__ void repeat(F &&f) {
+    if constexpr (N > 0) {
+        f();
+        repeat<N - 1>(f);
+    }
+}
+
+// Loads at a number of bytes in 32 bits from one address: no arithmetic in 64.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t near_of(const char *at) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at), 0, 0xffffffffu, 0x00020000);
+}
+__device__ __forceinline__ u32x4 load_near(__amdgpu_buffer_rsrc_t at, uint32_t byte) { return __builtin_amdgcn_raw_buffer_load_b128(at, (int)byte, 0, 0); }
+
 template <typename T, bool E4M3, int D, bool SCORED = false>
 __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(const ArgsOf<SCORED> a) {
     constexpr int KT = kManyRowsTile;
@@ -664,12 +717,11 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
     constexpr int CH = D / 16, DB = D / 32;                         // steps of the first product; blocks of the output
     static_assert(KT % RP == 0 && KT == 64, "whole pieces; a key a lane");
     constexpr bool kNarrow = E4M3 && T::kExponent == F16::kExponent;    // some scales do not go into T
-    // Pieces of 16 bytes are turned by their row's number so that the 16 rows that lanes read of K together, and the 4 rows by 64 bytes of V, lie in
-    // different banks (256 bytes of them): rows of 128 bytes take half of these each.
-    auto k_turn = [](uint32_t r) { return D == 128 ? r & 15 : r >> 1 & 7; };
-    auto v_turn = [](uint32_t r) { return D == 128 ? (r & 3) << 2 | (r & 1) : (r >> 1 & 1) * 5; };
-    __shared__ __attribute__((aligned(16))) char lds[2][2][KT * RB];
-    __shared__ uint32_t odd_tile[3];
+    // Rows lie further apart than they are long, so that the 16 rows that lanes read of K together, and the 4 rows by 64 bytes of V, are in different
+    // banks (256 bytes of them), while all that a lane reads lies at constants from one address.
+    constexpr int KB = RB + 16, VB = RB + 64;
+    __shared__ __attribute__((aligned(16))) char lds[2][KT * (KB + VB)];
+    __shared__ uint32_t odd_tile[2];                                // the number, from 1 on, of a tile with infinities or NaN among its values
     typedef typename T::x8 x8;
 
     const AttnItem it = a.items[blockIdx.x / a.kv_heads];
@@ -677,6 +729,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 32, h = lane / 32;
     const uint32_t row_pitch = a.kv_heads * PR * 16;
     const char *k_head = a.k + head * PR * 16, *v_head = a.v + head * PR * 16;
+    const __amdgpu_buffer_rsrc_t k_near = near_of(k_head), v_near = near_of(v_head);
     const uint32_t fetched = threadIdx.x / PR, piece = threadIdx.x % PR;
 
     const uint32_t rows_before = wave * 32;
@@ -685,6 +738,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
     // what the workgroup's rows see, and the wavefront's
     const RowsSee all_see = rows_see<SCORED>(a, it, it.first_row, it.first_row + it.n_rows - 1);
     const RowsSee see = rows_see<SCORED>(a, it, it.first_row + min(rows_before, it.n_rows - 1), it.first_row + min(rows_before + 31, it.n_rows - 1));
+    const Whole all_whole(it, all_see, KT), wave_whole(it, see, KT);
     const Seen seen = seen_from(it, bounds_of<SCORED>(a, it, row));
     const uint32_t w0 = it.hit + (it.first_row + min(rows_before, it.n_rows - 1)) / a.group;
     Bias bias{};
@@ -704,35 +758,48 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
 
     u32x4 kr[N], vr[N];
     Scales scales{};
-    uint32_t rows = 0;                          // of the tile on its way, a lane each
     auto fetch = [&](const KeyPlace &at) {
-        rows = at.block * a.block_tokens + at.row_in_block;
+        const uint32_t rows = at.block * a.block_tokens + at.row_in_block;
         if (E4M3) scales = load_scales(a, at.block, head);
+        // (what lane i RP + fetched has)
+        auto of_row = [&](uint32_t x, int i) { return (uint32_t)__builtin_amdgcn_ds_bpermute((int)(4 * fetched) + 4 * i * RP, (int)x); };
+        if (a.near) {
+            const uint32_t byte = rows * row_pitch;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const uint64_t from = (uint64_t)__shfl(rows, i * RP + fetched) * row_pitch + piece * 16;
-            kr[i] = *reinterpret_cast<const u32x4 *>(k_head + from);
-            vr[i] = *reinterpret_cast<const u32x4 *>(v_head + from);
+            for (int i = 0; i < N; ++i) {
+                const uint32_t from = of_row(byte, i) + piece * 16;
+                kr[i] = load_near(k_near, from);
+                vr[i] = load_near(v_near, from);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const uint64_t from = (uint64_t)of_row(rows, i) * row_pitch + piece * 16;
+                kr[i] = *reinterpret_cast<const u32x4 *>(k_head + from);
+                vr[i] = *reinterpret_cast<const u32x4 *>(v_head + from);
+            }
         }
     };
-    // Where a lane reads the first of its 16 bytes of K, and of its 8 of V, of a tile: the others are there with bits turned.
-    uint32_t k_at = n * RB + ((h ^ k_turn(n)) << 4);
-    uint32_t v_at = (4 * h + lane % 16 / 4) * RB + (((2 * (lane / 16 % 2) + lane % 4 / 2) ^ v_turn(lane % 16 / 4)) << 4) + lane % 2 * 8;
-    if (threadIdx.x < 3) odd_tile[threadIdx.x] = 0;
+    // Where a lane writes the first of its pieces, and reads the first of its 16 bytes of K and of its 8 of V, of a tile.
+    const uint32_t k_to = fetched * KB + piece * (E4M3 ? 32 : 16), v_to = KT * KB + fetched * VB + piece * (E4M3 ? 32 : 16);
+    const uint32_t k_at = n * KB + 16 * h, v_at = KT * KB + (4 * h + lane % 16 / 4) * VB + 32 * (lane / 16 % 2) + 8 * (lane % 4);
+    if (threadIdx.x < 2) odd_tile[threadIdx.x] = 0;
     __syncthreads();
     const uint32_t tiles = (it.end - it.begin + KT - 1) / KT;
+    auto place_of_tile = [&](uint32_t tile) { return it.begin + in_order<SCORED>(a, tile, tiles) * KT; };
     KeyPlace next{};
     if (tiles) {
-        const KeyPlace first = find_key(a, it, it.begin + lane);
-        next = find_key(a, it, it.begin + KT + lane);
+        const KeyPlace first = find_key(a, it, place_of_tile(0) + lane);
+        next = find_key(a, it, place_of_tile(1) + lane);
         fetch(first);
     }
     for (uint32_t tile = 0; tile < tiles; ++tile) {
-        const uint32_t v0 = it.begin + tile * KT;
-        char *k_lds = lds[tile % 2][0], *v_lds = lds[tile % 2][1];
+        const uint32_t v0 = place_of_tile(tile);
+        char *to = lds[tile % 2];
         // (infinities and NaN among values that not all rows see: as in the kernel above)
-        if (!all_seen(it, all_see, v0, v0 + KT - 1) && odd_pieces<T, E4M3>(vr)) {
-            odd_tile[tile % 3] = 1;
+        const bool common = all_whole(v0);
+        if (!common && odd_pieces<T, E4M3>(vr)) {
+            odd_tile[tile % 2] = tile + 1;
             make_plain<T, E4M3>(vr);
         }
         const Scales by{in_range(scales.k), in_range(scales.v)};
@@ -747,19 +814,18 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
                 const uint32_t r = i * RP + fetched;
                 u32x4 x, y;
                 codes_to_half<TK, E4M3>(kr[i], __shfl(times.k, (int)r), &x, &y);
-                *reinterpret_cast<u32x4 *>(k_lds + r * RB + (((2 * piece) ^ k_turn(r)) << 4)) = x;
-                *reinterpret_cast<u32x4 *>(k_lds + r * RB + (((2 * piece + 1) ^ k_turn(r)) << 4)) = y;
+                *reinterpret_cast<u32x4 *>(to + k_to + i * RP * KB) = x;
+                *reinterpret_cast<u32x4 *>(to + k_to + i * RP * KB + 16) = y;
                 codes_to_half<TV, E4M3>(vr[i], __shfl(times.v, (int)r), &x, &y);
-                *reinterpret_cast<u32x4 *>(v_lds + r * RB + (((2 * piece) ^ v_turn(r)) << 4)) = x;
-                *reinterpret_cast<u32x4 *>(v_lds + r * RB + (((2 * piece + 1) ^ v_turn(r)) << 4)) = y;
+                *reinterpret_cast<u32x4 *>(to + v_to + i * RP * VB) = x;
+                *reinterpret_cast<u32x4 *>(to + v_to + i * RP * VB + 16) = y;
             }
         };
         if (!E4M3) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const uint32_t r = i * RP + fetched;
-                *reinterpret_cast<u32x4 *>(k_lds + r * RB + ((piece ^ k_turn(r)) << 4)) = kr[i];
-                *reinterpret_cast<u32x4 *>(v_lds + r * RB + ((piece ^ v_turn(r)) << 4)) = vr[i];
+                *reinterpret_cast<u32x4 *>(to + k_to + i * RP * KB) = kr[i];
+                *reinterpret_cast<u32x4 *>(to + v_to + i * RP * VB) = vr[i];
             }
         } else if (apart) {
             convert(T{}, Bf16{}, Scales{1.f, 1.f});
@@ -768,16 +834,14 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
         }
         if (tile + 1 < tiles) {
             fetch(next);
-            if (tile + 2 < tiles) next = find_key(a, it, v0 + 2 * KT + lane);
+            if (tile + 2 < tiles) next = find_key(a, it, place_of_tile(tile + 2) + lane);
         }
         __syncthreads();
-        const bool odd = odd_tile[tile % 3] != 0;
-        if (threadIdx.x == 0) odd_tile[(tile + 2) % 3] = 0;
-
-        asm volatile("" : "+v"(k_at), "+v"(v_at));      // (the addresses made of them are made anew for each tile: registers are short)
+        const bool odd = !common && odd_tile[tile % 2] == tile + 1;
+        const bool whole = wave_whole(v0);
         // a tile that none of the wavefront's rows sees
-        if (!works || none_seen(it, see, v0, min(v0 + KT, it.end) - 1)) continue;
-        const bool whole = all_seen(it, see, v0, v0 + KT - 1);
+        if (!works || (!whole && none_seen(it, see, v0, min(v0 + KT, it.end) - 1))) continue;
+        const char *k_here = lds[tile % 2] + k_at, *v_here = lds[tile % 2] + v_at;
 
         // scores: lane (n, h) gets row n's of keys 32 b + 8 (i / 4) + 4 h + i % 4
         f32x16 s[2];
@@ -787,10 +851,16 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
             for (int i = 0; i < 16; ++i) s[b][i] = 0;
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
-                const x8 k = *reinterpret_cast<const x8 *>(k_lds + 32 * b * RB + (k_at ^ j << 5));
+                const x8 k = *reinterpret_cast<const x8 *>(k_here + 32 * b * KB + 32 * j);
                 s[b] = T::mma32(k, q[j], s[b]);
             }
         }
+        in_turn<kLdsReads, 4>();
+        repeat<2 * CH - 4>([] {
+            in_turn<kMatrix, 1>();
+            in_turn<kLdsReads, 1>();
+        });
+        in_turn<kMatrix, 4>();
         // what the lane of key `key` + 4 h has (its address made anew each time, too)
         auto of_key = [&](float x, int key) {
             int at = (int)(16 * h);
@@ -814,13 +884,14 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
                 more = a.cap;
             }
             if (a.slopes) {
-                const float slope = bias.slope * a.over;
+                float slope = bias.slope * a.over;
+                uint32_t key = n;
+                asm volatile("" : "+v"(slope), "+v"(key));      // (operands made anew for each tile: registers are short)
                 if (is_line(it, see, v0, KT, w0)) {
-                    more += line_begin(it, bias, v0) + bias.slope * (float)(4 * h);
+                    more += line_begin(it, bias, v0);
+                    const u32x2 parts = slope_parts(slope, h == 0);
 #pragma unroll
-                    for (int b = 0; b < 2; ++b)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) s[b][i] = __builtin_fmaf(slope, (float)(32 * b + 8 * (i / 4) + i % 4), s[b][i]);
+                    for (int b = 0; b < 2; ++b) s[b] = Bf16::add32(key_parts(32 * b + key, h == 0), parts, s[b]);
                 } else {
 #pragma unroll
                     for (int b = 0; b < 2; ++b)
@@ -862,8 +933,8 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
             return f32x2{x, y};
         };
         auto values = [&](int u, int d) {
-            const char *at = v_lds + 16 * u * RB + (v_at ^ d << 6);
-            const u32x2 x = read_columns16(at), y = read_columns16(at + 8 * RB);
+            const char *at = v_here + 16 * u * VB + 64 * d;
+            const u32x2 x = read_columns16(at), y = read_columns16(at + 8 * VB);
             return u32x4{x[0], x[1], y[0], y[1]};
         };
         // outputs: lane (n, h) gets row n's elements 32 d + 8 (i / 4) + 4 h + i % 4
@@ -892,21 +963,28 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
             for (int d = 0; d < DB; ++d) asm volatile("" : "+v"(o[d]));
         }
         if (!apart) {
-            x8 p[4];
+            // (the weights of the next 16 keys beside the matrix instructions of these)
+            u32x4 w, v[DB];
+            auto weigh = [&](int u, int i) {
+                const f32x2 x = weights(u, i);
+                w[i / 2] = narrow<T>(x[0], x[1]);
+            };
+#pragma unroll
+            for (int d = 0; d < DB; ++d) v[d] = values(0, d);
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) weigh(0, i);
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                u32x4 w;
+                const x8 p = __builtin_bit_cast(x8, w);
 #pragma unroll
-                for (int i = 0; i < 8; i += 2) {
-                    const f32x2 x = weights(u, i);
-                    w[i / 2] = narrow<T>(x[0], x[1]);
+                for (int d = 0; d < DB; ++d) {
+                    o[d] = T::mma32(__builtin_bit_cast(x8, v[d]), p, o[d]);
+                    if (u == 3) continue;
+                    v[d] = values(u + 1, d);
+#pragma unroll
+                    for (int i = 8 / DB * d; i < 8 / DB * (d + 1); i += 2) weigh(u + 1, i);
                 }
-                p[u] = __builtin_bit_cast(x8, w);
             }
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int d = 0; d < DB; ++d) o[d] = T::mma32(__builtin_bit_cast(x8, values(u, d)), p[u], o[d]);
         }
         if (odd) {
             for (uint32_t j = 0; j < KT && v0 + j < it.end; ++j) {

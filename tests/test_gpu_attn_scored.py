@@ -180,6 +180,24 @@ def test_a_bias_over_far_keys():
     close(b, *attend(b), b.want())
 
 
+@pytest.mark.parametrize("blocks", [(1 << 19) - 1, 1 << 19, (1 << 19) + 9])
+@pytest.mark.parametrize("slopes", [False, True])
+def test_planes_around_4_gib(blocks, slopes):
+    """The last blocks of planes of 2^32 bytes, one block less and some more: what a small pool gives, bit for bit (addresses in 32 and 64 bits)."""
+    b = Scored([70, 0, 5], [90, 200, 1], 64, (2, 1), 64, slopes=slopes)
+    want = attend(b)
+    small = b.planes()
+    first = blocks - small[0].shape[0]
+    planes = [torch.empty(blocks, *x.shape[1:], dtype=x.dtype, device="cuda") for x in small]
+    for x, y in zip(planes, small):
+        x[first:] = y
+    layout = K.make_attn_layout(64, 2, 1, 64, blocks, b.dtype)
+    p = K.kvl_attn_plan(layout, b.hit, b.app, [t + np.int32(first) for t in b.tables], K.KVL_GATHER | K.KVL_TOKENS_ALL)
+    got = attend(b, p, planes=planes)
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+
+
 def test_one_output_twice_and_on_another_stream():
     """Two plans' calls on two streams at once, each with a workspace of its own."""
     b = Scored([3000, 100], [2, 40], 16, (8, 2), 128, cap=6.0, prefix=[10, 120])
