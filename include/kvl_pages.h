@@ -83,9 +83,9 @@ typedef struct {
 int kvl_page_pools(const kvl_page_layout_t *layout, void *const *planes, uint32_t flags, kvl_page_pools_t **out);
 /* As kvl_plan_destroy: does not wait for the device. */
 void kvl_page_pools_destroy(kvl_page_pools_t *pools);
-/* Copy blocks of every layer and plane (copies: host array, borrowed for the call).  KVL_ERANGE: a block outside the pool, or blocks of more than 2^35 bytes over
- * all layers; KVL_EALIAS: a block is the destination of two copies, or of one and the source of one.  Takes no device memory, and can be captured into a HIP graph, which then repeats these
- * copies. */
+/* Copy blocks of every layer and plane (copies: host array, borrowed for the call).  KVL_ERANGE: a block outside the pool, or one whose layers and planes are
+ * more than 2^35 bytes together (2^33 where planes begin at multiples of 4 bytes, 2^31 where at any); KVL_EALIAS: a block is the destination of two copies, or
+ * of one and the source of one.  Takes no device memory, and can be captured into a HIP graph, which then repeats these copies. */
 int kvl_copy_blocks(const kvl_page_pools_t *pools, const kvl_block_copy_t *copies, uint64_t n, void *stream);
 
 #ifdef __cplusplus

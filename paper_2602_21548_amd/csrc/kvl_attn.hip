@@ -56,6 +56,8 @@ static int attn_layer(const kvl_attn_plan_t *plan, const kvl_attn_t *in, const k
     const kvl_attn_scores_t how = scores ? *scores : kvl_attn_scores_t{};
     // (a cap beyond 2^10 would leave small scores too few of the bits that a tanh in 32 bits has; NaN fails both)
     if (how.cap != 0 && !(how.cap >= 0x1p-10f && how.cap <= 0x1p10f)) return KVL_EINVAL;
+    // (a bias is added to scores before they are multiplied by the scale: as a slope over it)
+    if (how.slopes && how.cap == 0 && !(t.scale >= 0x1p-64f && t.scale <= 0x1p64f)) return KVL_EINVAL;
     int rc = check_attn_pool(plan, planes);
     if (rc != KVL_OK || plan->new_tokens == 0) return rc;
     const uint64_t n = plan->new_tokens, row = (uint64_t)l.q_heads * l.head_dim;

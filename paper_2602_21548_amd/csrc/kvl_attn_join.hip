@@ -122,5 +122,9 @@ static int attn_join(const kvl_attn_plan_t *plan, const kvl_attn_join_t *in, hip
 }  // namespace kvl
 
 extern "C" int kvl_attn_join(const kvl_attn_plan_t *plan, const kvl_attn_join_t *args, void *stream) {
-    return kvl::attn_join(plan, args, static_cast<hipStream_t>(stream));
+    try {
+        return kvl::attn_join(plan, args, static_cast<hipStream_t>(stream));
+    } catch (const std::exception &) {
+        return KVL_ENOMEM;
+    }
 }

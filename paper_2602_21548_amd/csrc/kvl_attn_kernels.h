@@ -320,6 +320,7 @@ __device__ __forceinline__ void write_lse(const AttnArgs &a, uint32_t token0, ui
 // Beyond 32 rows the registers do not hold a wavefront's outputs beside what is on its way, and scratch memory's loads come in order behind those of
 // the next keys: there HALVES = 2, and two wavefronts take the same tile of keys, half of the rows each; what the second one loads is in the caches.
 // (32 requests of 21 to 42 rows, 8-bit heads of 128: 59 us with three tiles of rows a wavefront and five such loads for each of keys, 51 so.)
+// (SCORED instances of one tile of rows over an 8-bit cache have registers for three wavefronts a SIMD only where that is asked for: as the others have.)
 template <typename T, bool E4M3, int D, int RT, int HALVES, bool SCORED = false>
 __global__ void __launch_bounds__(256, SCORED && E4M3 && RT == 1 ? 3 : 2) kvl_attn_few_kernel(const ArgsOf<SCORED> a) {
     constexpr int KT = few_rows_tile(D), NB = KT / 16;        // keys of a tile, blocks of 16

@@ -457,8 +457,16 @@ struct Array {
     T *as() const { return (T *)view.buf; }
 };
 void *handle_of(PyObject *o) { return PyLong_AsVoidPtr(o); }     // (0 where it is no number: the library refuses it)
-#define KVL_ARRAY(name, at, type, write)                                                                                 Array name;                                                                                                          if (!name.get(a[at], sizeof(type), write)) return nullptr
-#define KVL_PAGES(count)                                                                                                 if (n != count) {                                                                                                        PyErr_SetString(PyExc_TypeError, "wrong number of arguments");                                                       return nullptr;                                                                                                  }                                                                                                                    void *pages = handle_of(a[0]);                                                                                       if (PyErr_Occurred()) return nullptr
+#define KVL_ARRAY(name, at, type, write) \
+    Array name;                          \
+    if (!name.get(a[at], sizeof(type), write)) return nullptr
+#define KVL_PAGES(count)                                                   \
+    if (n != count) {                                                      \
+        PyErr_SetString(PyExc_TypeError, "wrong number of arguments");     \
+        return nullptr;                                                    \
+    }                                                                      \
+    void *pages = handle_of(a[0]);                                         \
+    if (PyErr_Occurred()) return nullptr
 
 PyObject *pages_fork(PyObject *, PyObject *const *a, Py_ssize_t n) {        // handle, sequences, numbers of the forks
     KVL_PAGES(3);

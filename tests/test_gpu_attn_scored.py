@@ -256,6 +256,10 @@ def test_refusals():
         with pytest.raises(K.KvlError) as e:
             K.kvl_attn_layer(p, q, planes, out, ws, cap=cap)
         assert e.value.code == K.KVL_EINVAL
+    for scale in (2.0 ** -65, 2.0 ** 65):
+        with pytest.raises(K.KvlError) as e:
+            K.kvl_attn_layer(p, q, planes, out, ws, scale=scale, slopes=b.slopes.cuda())
+        assert e.value.code == K.KVL_EINVAL
     for slopes in (torch.zeros(4), torch.zeros(5, device="cuda"), torch.zeros(4, device="cuda").double(), torch.zeros(2, 2, device="cuda"), [0.1] * 4,
                    torch.zeros(8, device="cuda")[::2]):
         with pytest.raises((ValueError, TypeError)):
