@@ -806,7 +806,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) kvl_attn_many_kernel(con
         const Scales by{in_range(scales.k), in_range(scales.v)};
         // (the same in all wavefronts: each has every key's scales)
         const bool apart = kNarrow && __builtin_amdgcn_readfirstlane(__any(!suits_f16(by.k) || !suits_f16(by.v)));
-        // (one branch around all of it: 32-K tails in fp16 784 us, one at each value 812, without the second form 768)
+        // (one branch around all of it: where 32-K tails in fp16 took 784 us, one at each value 812, without the second form 768; 719 now)
         auto convert = [&](auto key_type, auto value_type, Scales times) {
             typedef decltype(key_type) TK;
             typedef decltype(value_type) TV;
