@@ -73,6 +73,8 @@ struct kvl_pages_s {
     std::vector<kvl::Sequence> sequences;       // by the number's lower half
     std::vector<uint32_t> slots;                // of those that have ended, with room for all
     uint32_t stamp = 0;
+    std::vector<uint32_t> named;                // of each block, once a table was adopted: by which one last
+    uint32_t naming = 0;
 
     kvl_pages_s(uint32_t bs, uint64_t n) : block_tokens(bs), pool_blocks(n), free(n), users(n, 0) {}
 
@@ -96,6 +98,20 @@ struct kvl_pages_s {
             s->stamp = stamp;
         }
         return true;
+    }
+    // Whether these are blocks of the pool (KVL_ERANGE), and none is there twice (KVL_EALIAS).
+    int check_table(const int32_t *table, uint64_t n) {
+        if (n && named.empty()) named.resize(pool_blocks, 0);
+        if (++naming == 0) {
+            std::fill(named.begin(), named.end(), 0u);
+            naming = 1;
+        }
+        for (uint64_t i = 0; i < n; ++i) {
+            if (table[i] < 0 || (uint64_t)table[i] >= pool_blocks) return KVL_ERANGE;
+            if (named[(size_t)table[i]] == naming) return KVL_EALIAS;
+            named[(size_t)table[i]] = naming;
+        }
+        return KVL_OK;
     }
     // Room for n new sequences: nothing is allocated by their making, or by their end.
     void make_room(uint32_t n) {
@@ -155,17 +171,12 @@ int guarded(F &&f) {
 
 int adopt(kvl_pages_t *pages, const kvl_request_t *req, uint32_t n, uint64_t *out) {
     std::vector<std::vector<int32_t>> tables(n);
-    std::vector<uint32_t> seen(pages->pool_blocks, 0);
     for (uint32_t i = 0; i < n; ++i) {
         const uint64_t tokens = (uint64_t)req[i].hit_tokens + req[i].append_tokens, blocks = pages->blocks_of(tokens);
         if (tokens >= kMostTokens || req[i].n_blocks < blocks) return KVL_ERANGE;
         if (blocks && !req[i].block_table) return KVL_EINVAL;
-        for (uint64_t b = 0; b < blocks; ++b) {
-            const int32_t id = req[i].block_table[b];
-            if (id < 0 || (uint64_t)id >= pages->pool_blocks) return KVL_ERANGE;
-            if (seen[(size_t)id] == i + 1) return KVL_EALIAS;
-            seen[(size_t)id] = i + 1;
-        }
+        const int rc = pages->check_table(req[i].block_table, blocks);
+        if (rc != KVL_OK) return rc;
         if (blocks) tables[i].assign(req[i].block_table, req[i].block_table + blocks);
     }
     pages->make_room(n);
