@@ -121,9 +121,12 @@ class PagePools(_Owner):
         self.planes = planes
 
 
+_UINT64, _UINT32, _INT32 = np.dtype(np.uint64), np.dtype(np.uint32), np.dtype(np.int32)
+
+
 def _numbers(x, dtype, what: str) -> np.ndarray:
     """A contiguous array of whole numbers of this type."""
-    if type(x) is np.ndarray and x.dtype == dtype and x.ndim == 1 and x.flags.c_contiguous:
+    if type(x) is np.ndarray and x.dtype is dtype and x.ndim == 1 and x.flags.c_contiguous:
         return x
     most = int(np.iinfo(dtype).max)
     try:
@@ -136,16 +139,20 @@ def _numbers(x, dtype, what: str) -> np.ndarray:
 
 
 def _sequences(x, what: str) -> np.ndarray:
-    return _numbers(x, np.uint64, f"{what} sequences")
+    if type(x) is np.ndarray and x.dtype is _UINT64 and x.ndim == 1 and x.flags.c_contiguous:
+        return x
+    return _numbers(x, _UINT64, f"{what} sequences")
 
 
 def _per_sequence(tokens, n: int, what: str) -> np.ndarray:
     """One number for all sequences, or one for each."""
     if type(tokens) is int and 0 <= tokens < 1 << 32:
-        return np.full(n, tokens, dtype=np.uint32)
+        out = np.empty(n, dtype=_UINT32)
+        out.fill(tokens)
+        return out
     if isinstance(tokens, (int, np.integer)):
         tokens = [int(tokens)] * n
-    tokens = _numbers(tokens, np.uint32, f"{what} tokens")
+    tokens = _numbers(tokens, _UINT32, f"{what} tokens")
     if tokens.size != n:
         raise ValueError(f"{what}: need tokens for every sequence")
     return tokens
@@ -173,7 +180,7 @@ def kvl_pages_adopt(pages: Pages, tables: Sequence[np.ndarray], tokens) -> np.nd
 def kvl_pages_fork(pages: Pages, sequences) -> np.ndarray:
     """New sequences that are what these are now; their numbers."""
     s = _sequences(sequences, "kvl_pages_fork")
-    out = np.empty(s.size, dtype=np.uint64)
+    out = np.empty(s.size, dtype=_UINT64)
     _b._check(_fork(pages.handle, s, out), "kvl_pages_fork")
     return out
 
@@ -183,7 +190,7 @@ def kvl_pages_extend(pages: Pages, sequences, tokens) -> np.ndarray:
     int32 [copies, 2], from and to."""
     s = _sequences(sequences, "kvl_pages_extend")
     t = _per_sequence(tokens, s.size, "kvl_pages_extend")
-    copies = np.empty((s.size, 2), dtype=np.int32)
+    copies = np.empty((s.size, 2), dtype=_INT32)
     n = _extend(pages.handle, s, t, copies)
     if n < 0:
         _b._check(n, "kvl_pages_extend")
@@ -219,7 +226,7 @@ def kvl_pages_compact(pages: Pages, most: int = None) -> np.ndarray:
 def kvl_pages_tables(pages: Pages, sequences) -> List[np.ndarray]:
     """The block table of each sequence (int32; parts of one array)."""
     s = _sequences(sequences, "kvl_pages_tables")
-    first, table = np.empty(s.size + 1, dtype=np.uint64), np.empty(pages._longest, dtype=np.int32)
+    first, table = np.empty(s.size + 1, dtype=_UINT64), np.empty(pages._longest, dtype=_INT32)
     rc = _tables(pages.handle, s, table, first)
     if rc == _b.KVL_ESPACE:
         table = np.empty(int(first[-1]), dtype=np.int32)
@@ -267,7 +274,7 @@ def kvl_page_pools(block_bytes: Sequence[int], pool_blocks: int, pools: Sequence
 def kvl_copy_blocks(pools: PagePools, copies, stream=None) -> None:
     """Copy blocks of every layer and plane: int32 [copies, 2], from and to.  No block may be the destination of two, or of one and the source of one."""
     c = copies
-    if not (type(c) is np.ndarray and c.dtype == np.int32 and c.ndim == 2 and c.shape[1] == 2 and c.flags.c_contiguous):
+    if not (type(c) is np.ndarray and c.dtype is _INT32 and c.ndim == 2 and c.shape[1] == 2 and c.flags.c_contiguous):
         c = np.asarray(copies)
         if c.size == 0:
             c = np.empty((0, 2), dtype=np.int32)
