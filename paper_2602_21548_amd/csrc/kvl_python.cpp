@@ -56,6 +56,7 @@ struct Library {
     decltype(&kvl_pages_free) end;
     decltype(&kvl_pages_tables) tables;
     decltype(&kvl_copy_blocks) copy_blocks;
+    decltype(&kvl_pages_compact) compact;
 } g_lib;
 PyObject *g_float32;
 PyObject *g_tensor_type, *g_array_type, *g_raw_stream, *g_get_device, *g_is_initialized;
@@ -487,6 +488,13 @@ PyObject *pages_extend(PyObject *, PyObject *const *a, Py_ssize_t n) {
                                 copies.as<kvl_block_copy_t>(), &made);
     return PyLong_FromLong(rc != KVL_OK ? rc : (long)made);
 }
+PyObject *pages_compact(PyObject *, PyObject *const *a, Py_ssize_t n) {     // handle, copies; as above
+    KVL_PAGES(2);
+    KVL_ARRAY(copies, 1, int32_t, true);
+    uint32_t made = 0;
+    const int rc = g_lib.compact((kvl_pages_t *)pages, (uint32_t)(copies.size() / 2), copies.as<kvl_block_copy_t>(), &made);
+    return PyLong_FromLong(rc != KVL_OK ? rc : (long)made);
+}
 PyObject *pages_free(PyObject *, PyObject *const *a, Py_ssize_t n) {        // handle, sequences
     KVL_PAGES(2);
     KVL_ARRAY(sequences, 1, uint64_t, false);
@@ -509,10 +517,11 @@ PyObject *copy_blocks(PyObject *, PyObject *const *a, Py_ssize_t n) {       // h
     KVL_CALL(g_lib.copy_blocks((const kvl_page_pools_t *)pages, copies.as<kvl_block_copy_t>(), copies.size() / 2, s));
 }
 
-// setup_pages(the addresses of the pages' five entry points)
+// setup_pages(the addresses of the pages' six entry points)
 PyObject *setup_pages(PyObject *, PyObject *args) {
-    unsigned long long f[5];
-    if (!PyArg_ParseTuple(args, "KKKKK", &f[0], &f[1], &f[2], &f[3], &f[4])) return nullptr;
+    unsigned long long f[6];
+    if (!PyArg_ParseTuple(args, "KKKKKK", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5])) return nullptr;
+    g_lib.compact = (decltype(g_lib.compact))(uintptr_t)f[5];
     g_lib.fork = (decltype(g_lib.fork))(uintptr_t)f[0];
     g_lib.extend = (decltype(g_lib.extend))(uintptr_t)f[1];
     g_lib.end = (decltype(g_lib.end))(uintptr_t)f[2];
@@ -673,6 +682,7 @@ PyMethodDef module_methods[] = {
     {"setup_attn", setup_attn, METH_VARARGS, nullptr},
     {"pages_fork", (PyCFunction)(void (*)(void))pages_fork, METH_FASTCALL, nullptr},
     {"pages_extend", (PyCFunction)(void (*)(void))pages_extend, METH_FASTCALL, nullptr},
+    {"pages_compact", (PyCFunction)(void (*)(void))pages_compact, METH_FASTCALL, nullptr},
     {"pages_free", (PyCFunction)(void (*)(void))pages_free, METH_FASTCALL, nullptr},
     {"pages_tables", (PyCFunction)(void (*)(void))pages_tables, METH_FASTCALL, nullptr},
     {"copy_blocks", (PyCFunction)(void (*)(void))copy_blocks, METH_FASTCALL, nullptr},

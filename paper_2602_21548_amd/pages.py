@@ -56,6 +56,11 @@ def _extend(pages: int, s: np.ndarray, tokens: np.ndarray, copies: np.ndarray) -
     return _lib.kvl_pages_extend(pages, s.ctypes.data, tokens.ctypes.data, s.size, copies.ctypes.data, C.byref(n)) or n.value
 
 
+def _compact(pages: int, copies: np.ndarray) -> int:
+    n = C.c_uint32()
+    return _lib.kvl_pages_compact(pages, copies.shape[0], copies.ctypes.data, C.byref(n)) or n.value
+
+
 def _free(pages: int, s: np.ndarray) -> int:
     return _lib.kvl_pages_free(pages, s.ctypes.data, s.size)
 
@@ -68,8 +73,9 @@ _copy = _b._not_taken
 if _b._native is not None:
     # (by ctypes a call takes some microseconds more)
     _b._native.setup_pages(*(C.cast(getattr(_lib, f), C.c_void_p).value
-                             for f in ("kvl_pages_fork", "kvl_pages_extend", "kvl_pages_free", "kvl_pages_tables", "kvl_copy_blocks")))
+                             for f in ("kvl_pages_fork", "kvl_pages_extend", "kvl_pages_free", "kvl_pages_tables", "kvl_copy_blocks", "kvl_pages_compact")))
     _fork, _extend, _free, _tables = _b._native.pages_fork, _b._native.pages_extend, _b._native.pages_free, _b._native.pages_tables
+    _compact = _b._native.pages_compact
     _copy = _b._native.copy_blocks
 
 
@@ -129,6 +135,10 @@ def _numbers(x, dtype, what: str) -> np.ndarray:
     if type(x) is np.ndarray and x.dtype is dtype and x.ndim == 1 and x.flags.c_contiguous:
         return x
     most = int(np.iinfo(dtype).max)
+    if type(x) is np.ndarray and x.ndim == 1 and x.dtype.kind in "iu":
+        if x.size and (int(x.min()) < 0 or int(x.max()) > most):
+            raise ValueError(f"{what}: need whole numbers from 0 to {most}")
+        return np.ascontiguousarray(x, dtype=dtype)
     try:
         x = [operator.index(v) for v in x]      # (NumPy makes floats of uint64 numbers beside others)
     except TypeError:
@@ -213,14 +223,16 @@ def kvl_pages_free(pages: Pages, sequences) -> None:
 def kvl_pages_compact(pages: Pages, most: int = None) -> np.ndarray:
     """Blocks in use move to the front of the pool, at most so many (all by default).  The copies, int32 [copies, 2], from and to, which have to be made
     before anything else is written."""
-    moves = kvl_pages_stats(pages)["moves"]
+    moves = pages.pool_blocks // 2              # (as many blocks in use as free ones change places, at most)
     if most is not None:
         if int(most) < 0:
             raise ValueError(f"kvl_pages_compact: most is {most}")
         moves = min(moves, int(most))
-    copies, n = np.empty((moves, 2), dtype=np.int32), C.c_uint32()
-    _b._check(_lib.kvl_pages_compact(pages.handle, moves, copies.ctypes.data, C.byref(n)), "kvl_pages_compact")
-    return copies[:n.value]
+    copies = np.empty((moves, 2), dtype=_INT32)
+    n = _compact(pages.handle, copies)
+    if n < 0:
+        _b._check(n, "kvl_pages_compact")
+    return copies[:n] if 4 * n > moves else copies[:n].copy()
 
 
 def kvl_pages_tables(pages: Pages, sequences) -> List[np.ndarray]:

@@ -227,3 +227,30 @@ def test_binding_and_header_agree(tmp_path):
     r = subprocess.run(["gcc", "-std=c99", "-pedantic", "-Wall", "-Wextra", "-Werror", "-I" + include, str(src), "-o", str(tmp_path / "c")],
                        capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
+
+
+@pytest.mark.parametrize("dtype", [np.int64, np.uint64, np.int32, np.uint16, ">i8"])
+def test_numbers_of_any_integer_type(dtype):
+    """And at any stride; what does not fit is refused, whichever form it has."""
+    pages = K.kvl_pages(4, 64)
+    s = K.kvl_pages_adopt(pages, [np.zeros(0, np.int32)] * 6, 0)
+    some = np.zeros(6, dtype=dtype)
+    some[::2] = s[:3]
+    K.kvl_pages_extend(pages, some[::2], np.array([5, 0, 9], dtype=dtype))
+    assert K.kvl_pages_tokens(pages, s.astype(dtype)).tolist() == [5, 0, 9, 0, 0, 0]
+    K.kvl_pages_truncate(pages, some[::2], np.array([1, 0, 8], dtype=dtype))
+    assert K.kvl_pages_tokens(pages, s[:3]).tolist() == [1, 0, 8]
+    for bad in (np.array([-1], dtype=np.int64), np.array([1 << 32], dtype=np.uint64), np.array([[1]]), np.array([1.0])):
+        with pytest.raises(ValueError):
+            K.kvl_pages_extend(pages, s[:1], bad)
+
+
+def test_a_long_pool_of_which_little_moves():
+    n = 100_000
+    pages = K.kvl_pages(1, n)
+    s = K.kvl_pages_adopt(pages, [np.array([n - 1, 3, n - 7], dtype=np.int32)], [3])
+    assert K.kvl_pages_compact(pages, 1).tolist() == [[n - 1, 0]]
+    copies = K.kvl_pages_compact(pages)
+    assert copies.tolist() == [[n - 7, 1], [3, 2]] and copies.base is None
+    assert K.kvl_pages_tables(pages, s)[0].tolist() == [0, 2, 1]
+    assert K.kvl_pages_compact(pages).shape == (0, 2) and K.kvl_pages_compact(K.kvl_pages(1, 1)).shape == (0, 2)
