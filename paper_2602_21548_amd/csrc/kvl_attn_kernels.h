@@ -176,10 +176,11 @@ __device__ __forceinline__ Seen seen_from(const AttnItem &it, const AttnBounds &
 // A row's bias: - slope |position - t|, slope times log2(e).
 //
 // In a tile that is a run of tokens, none of which a row sees before its position, that is slope (t0 - position) + slope k for the tile's first
-// token t0 and the number k of a key in it.  The first part is added once, to what is taken off all of a lane's exponents.  The second is a product of keys by
-// rows, which the matrix unit adds: k is a bf16 number, the slope three of them (24 bits; products and sums are in 32 bits as the scores' are).  Tiles in
-// which first tokens end, or of a prefix beyond a row's position, take each distance.  (Tails of 256 to 1024 tokens over 8 to 32 K keys, us: each distance
-// 1435, one operation with a constant a score 1198, the matrix unit 1179, without a bias 1020.)
+// token t0 and the number k of a key in it.  The first part is added once, to what is taken off all of a lane's exponents.  The second is one operation with a
+// constant a score in the kernel for few rows.  In that for many it is a product of keys by rows, which the matrix unit adds: k is a bf16 number, the slope three
+// of them (24 bits; products and sums are in 32 bits as the scores' are).  Tiles in which first tokens end, or of a prefix beyond a row's position, take each
+// distance.  (Tails of 256 to 1024 tokens over 8 to 32 K keys, us: each distance 1435, one operation a score 1198, the matrix unit 1179, without a bias
+// 1020; few rows are level.)
 struct Bias {
     float slope;
     uint32_t position;
@@ -501,10 +502,11 @@ __global__ void __launch_bounds__(256, SCORED && E4M3 && RT == 1 ? 3 : 2) kvl_at
                     if (a.slopes) {
                         const Bias bias = kStaged ? biases[((R0 + r) * HALVES + half) * 16 + n] : bias_here;
                         if (is_line(it, see, v0, KT, p0)) {
-                            more += line_begin(it, bias, v0);
-                            const u32x2 slope = slope_parts(bias.slope, g == 0);
+                            more += line_begin(it, bias, v0) + bias.slope * (float)(4 * g);
 #pragma unroll
-                            for (int b = 0; b < NB; ++b) s[r][b] = Bf16::add16(key_parts(16 * b + n, g == 0), slope, s[r][b]);
+                            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) s[r][b][i] = __builtin_fmaf(bias.slope, (float)(16 * b + i), s[r][b][i]);
                         } else {
 #pragma unroll
                             for (int b = 0; b < NB; ++b)
@@ -702,7 +704,8 @@ __device__ __forceinline__ void repeat(F &&f) {
     }
 }
 
-// Loads at a number of bytes in 32 bits from one address: no arithmetic in 64.
+// Loads at a number of bytes in 32 bits from one address: no arithmetic in 64, which planes of 4 GiB and more take.  (16-bit tails over 8 to 32 K keys: 1025 us
+// in 64 bits, 1000 so.)
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t near_of(const char *at) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at), 0, 0xffffffffu, 0x00020000);
 }

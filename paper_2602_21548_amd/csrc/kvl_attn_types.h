@@ -22,13 +22,10 @@ struct Bf16 {
     static __device__ __forceinline__ f32x2 widen(uint32_t w) { return f32x2{__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)}; }
     static __device__ __forceinline__ f32x16 mma32(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ f32x4 mma16(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-    // contractions of 8 and of 16, of which a lane has 4
-    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    // a contraction of 8, of which a lane has 4
     static __device__ __forceinline__ f32x16 add32(u32x2 a, u32x2 b, f32x16 c) {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
         return __builtin_amdgcn_mfma_f32_32x32x8bf16_1k(__builtin_bit_cast(s16x4, a), __builtin_bit_cast(s16x4, b), c, 0, 0, 0);
-    }
-    static __device__ __forceinline__ f32x4 add16(u32x2 a, u32x2 b, f32x4 c) {
-        return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, a), __builtin_bit_cast(s16x4, b), c, 0, 0, 0);
     }
     // two codes of e4m3 times 2 to the exponent of `scale`
     template <bool HI>
