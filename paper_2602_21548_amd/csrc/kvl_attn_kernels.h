@@ -433,7 +433,8 @@ __global__ void __launch_bounds__(256, SCORED && E4M3 && RT == 1 ? 3 : 2) kvl_at
         if (E4M3) {
             if (lane < KT) {
                 const float by = in_range(scales.v);
-                key_c[lane] = a.c * in_range(scales.k);
+                // (held to what floats hold: a product of 0 is a score of 0, whatever it is multiplied by)
+                key_c[lane] = fminf(a.c * in_range(scales.k), 3.40282347e38f);
                 key_log[lane] = __log2f(by);
                 key_over[lane] = __builtin_amdgcn_rcpf(by);        // (to a unit in the last place of 32 bits, as the sum it goes into)
             }
