@@ -290,7 +290,7 @@ def kvl_copy_blocks(pools: PagePools, copies, stream=None) -> None:
         c = np.asarray(copies)
         if c.size == 0:
             c = np.empty((0, 2), dtype=np.int32)
-        if c.ndim != 2 or c.shape[1] != 2 or (c.size and (c.dtype.kind not in "iu" or abs(c.astype(np.int64)).max() >= 1 << 31)):
+        if c.ndim != 2 or c.shape[1] != 2 or (c.size and (c.dtype.kind not in "iu" or int(c.min()) < -(1 << 31) or int(c.max()) >= 1 << 31)):
             raise ValueError("kvl_copy_blocks: copies must be whole numbers [copies, 2]")
         c = np.ascontiguousarray(c, dtype=np.int32)
     rc = _copy(pools.handle, c, stream)
