@@ -236,7 +236,7 @@ def kvl_pages_compact(pages: Pages, most: int = None) -> np.ndarray:
 
 
 def kvl_pages_tables(pages: Pages, sequences) -> List[np.ndarray]:
-    """The block table of each sequence (int32; parts of one array)."""
+    """The block table of each sequence (int32; parts of one array, of at most four times their entries, or of 64)."""
     s = _sequences(sequences, "kvl_pages_tables")
     first, table = np.empty(s.size + 1, dtype=_UINT64), np.empty(pages._longest, dtype=_INT32)
     rc = _tables(pages.handle, s, table, first)
@@ -246,6 +246,8 @@ def kvl_pages_tables(pages: Pages, sequences) -> List[np.ndarray]:
         rc = _tables(pages.handle, s, table, first)
     _b._check(rc, "kvl_pages_tables")
     at = first.tolist()
+    if table.size > 4 * max(at[-1], 16):        # (short tables do not keep the room of the longest ones that were asked for)
+        table = table[:at[-1]].copy()
     return [table[a:b] for a, b in zip(at, at[1:])]
 
 

@@ -18,3 +18,29 @@ class NoPools:
 def test_copies_of_blocks_that_32_bits_do_not_hold(copies):
     with pytest.raises(ValueError):
         K.kvl_copy_blocks(NoPools(), copies)
+
+
+def held(tables):
+    """Bytes that tables keep, by the arrays that they are parts of."""
+    bases = {}
+    for t in tables:
+        while t.base is not None:
+            t = t.base
+        bases[id(t)] = t.nbytes
+    return sum(bases.values())
+
+
+def test_short_tables_after_a_long_one_do_not_keep_its_room():
+    pages = K.kvl_pages(16, 300000)
+    long, short, none = K.kvl_pages_adopt(pages, [np.arange(250000), np.array([299999, 7, 250001]), np.array([], dtype=np.int32)], [16 * 250000, 37, 0])
+    for _ in range(3):
+        t = K.kvl_pages_tables(pages, [long])
+        assert held(t) <= 4 * 4 * 250000 and np.array_equal(t[0], np.arange(250000))
+        t = K.kvl_pages_tables(pages, [short, none, short])
+        assert [x.tolist() for x in t] == [[299999, 7, 250001], [], [299999, 7, 250001]] and all(x.dtype == np.int32 for x in t)
+        assert held(t) <= 4 * 4 * 6
+        assert held(K.kvl_pages_tables(pages, [none])) == 0 and K.kvl_pages_tables(pages, []) == []
+    # (and each call's are its own)
+    a, b = K.kvl_pages_tables(pages, [short]), K.kvl_pages_tables(pages, [short])
+    a[0][:] = 1
+    assert b[0].tolist() == [299999, 7, 250001]
