@@ -354,10 +354,19 @@ def make_layout(n_layers: int, block_tokens: int, row_bytes: Sequence[int], pool
     return lay
 
 
+def _whole(x, dtype) -> np.ndarray:
+    """An array of this type.  NumPy wraps whole numbers that it does not hold where they come in an array of another type: KVL_ERANGE."""
+    if isinstance(x, np.ndarray) and x.dtype != dtype and x.dtype.kind in "iu" and x.size:
+        info = np.iinfo(dtype)
+        if int(x.min()) < info.min or int(x.max()) > info.max:
+            raise KvlError(KVL_ERANGE, "requests")
+    return np.asarray(x, dtype=dtype)
+
+
 def _requests(hit, app, tables: Sequence[np.ndarray]):
     """(kvl_request_t array, n, arrays to keep alive while it is in use)"""
-    hit = np.asarray(hit, dtype=np.uint32)
-    app = np.asarray(app, dtype=np.uint32)
+    hit = _whole(hit, np.uint32)
+    app = _whole(app, np.uint32)
     n = int(hit.shape[0])
     if len(tables) != n or app.shape[0] != n:
         raise ValueError("hit, app and tables must have one entry per request")
@@ -365,7 +374,7 @@ def _requests(hit, app, tables: Sequence[np.ndarray]):
     keep = list(tables)         # (gone through once: it may not allow a second time)
     if _native is not None and _native.requests(hit, app, keep, reqs):
         return reqs, n, keep
-    keep = [np.ascontiguousarray(np.asarray(t, dtype=np.int32)) for t in keep]
+    keep = [np.ascontiguousarray(_whole(t, np.int32)) for t in keep]
     for r in range(n):
         reqs[r].hit_tokens = int(hit[r])
         reqs[r].append_tokens = int(app[r])

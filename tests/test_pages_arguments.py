@@ -44,3 +44,21 @@ def test_short_tables_after_a_long_one_do_not_keep_its_room():
     a, b = K.kvl_pages_tables(pages, [short]), K.kvl_pages_tables(pages, [short])
     a[0][:] = 1
     assert b[0].tolist() == [299999, 7, 250001]
+
+
+@pytest.mark.parametrize("table", [np.array([2 ** 32 + 1, 2]), np.array([2, -2 ** 32]), np.array([2 ** 63, 2], dtype=np.uint64), np.array([2 ** 32 - 1, 2], dtype=np.uint32)])
+def test_tables_of_blocks_that_32_bits_do_not_hold(table):
+    """Adopted, or of a plan: as other blocks outside the pool."""
+    pages = K.kvl_pages(16, 8)
+    layout, attn = K.make_layout(1, 16, [64], 8), K.make_attn_layout(16, 2, 1, 64, 8)
+    for call in (lambda: K.kvl_pages_adopt(pages, [np.array([0, 1]), table], [20, 20]), lambda: K.kvl_plan(layout, [20], [5], [table], K.KVL_GATHER | K.KVL_HOST_ONLY),
+                 lambda: K.kvl_attn_plan(attn, [20], [5], [table], K.KVL_GATHER | K.KVL_HOST_ONLY)):
+        with pytest.raises(K.KvlError) as e:
+            call()
+        assert e.value.code == K.KVL_ERANGE
+    assert K.kvl_pages_stats(pages)["sequences"] == 0
+    for hit, app in ((np.array([2 ** 32]), [5]), ([20], np.array([2 ** 32 + 5])), (np.array([-2 ** 32]), [5])):
+        with pytest.raises(K.KvlError) as e:
+            K.kvl_attn_plan(attn, hit, app, [np.array([1, 2])], K.KVL_GATHER | K.KVL_HOST_ONLY)
+        assert e.value.code == K.KVL_ERANGE
+    assert K.kvl_pages_adopt(pages, [np.array([5, 2]), [6, 1]], np.array([20, 20])).size == 2      # (other types hold what is in the pool)
