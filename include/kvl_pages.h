@@ -73,7 +73,7 @@ int kvl_pages_stats(const kvl_pages_t *pages, kvl_pages_stats_t *out);
 /* The planes of a pool that copies go through: a block of plane p has block_bytes[p] bytes in each layer (two of kvl_attn.h's 8-bit cache are
  * block_tokens * kv_heads * head_dim codes, two are 4 * kv_heads bytes of scales), block b at b * block_bytes[p].
  * planes: host array [n_layers][n_planes] of device pointers, borrowed for the call; the memory has to stay.
- * flags: KVL_NO_POINTER_CHECKS, KVL_CALLER_SYNCS, as in kvl_plan. */
+ * flags: KVL_NO_POINTER_CHECKS, KVL_CALLER_SYNCS, as in kvl_plan.  KVL_ERANGE: more than 2^31 - 1 blocks, or a block of a plane of more than 2^32 bytes. */
 typedef struct {
     uint32_t n_layers;                      /* up to 4096 */
     uint32_t n_planes;                      /* up to KVL_MAX_PLANES */
@@ -83,8 +83,9 @@ typedef struct {
 int kvl_page_pools(const kvl_page_layout_t *layout, void *const *planes, uint32_t flags, kvl_page_pools_t **out);
 /* As kvl_plan_destroy: does not wait for the device. */
 void kvl_page_pools_destroy(kvl_page_pools_t *pools);
-/* Copy blocks of every layer and plane (copies: host array, borrowed for the call).  KVL_ERANGE: a block outside the pool, or one whose layers and planes are
- * more than 2^35 bytes together (2^33 where planes begin at multiples of 4 bytes, 2^31 where at any); KVL_EALIAS: a block is the destination of two copies, or
+/* Copy blocks of every layer and plane (copies: host array, borrowed for the call).  KVL_ERANGE: a block outside the pool, or more than a launch holds: 2^32 lanes
+ * or more for one copy, where a plane of a layer takes a lane for each 16 bytes of a block (4 where its size, or where it begins in some layer, is a multiple
+ * of 4 and not of 16; 1 where it is of neither) and 256 more.  So up to nearly 2^36 bytes a copy (2^34, 2^32) are taken.  KVL_EALIAS: a block is the destination of two copies, or
  * of one and the source of one.  Takes no device memory, and can be captured into a HIP graph, which then repeats these copies. */
 int kvl_copy_blocks(const kvl_page_pools_t *pools, const kvl_block_copy_t *copies, uint64_t n, void *stream);
 

@@ -1,8 +1,11 @@
 """What the binding of a pool's pages takes and refuses, before anything of it goes to a device (host only)."""
+import ctypes as C
+
 import numpy as np
 import pytest
 
 import paper_2602_21548_amd as K
+from paper_2602_21548_amd import pages as P
 
 
 class NoPools:
@@ -62,3 +65,11 @@ def test_tables_of_blocks_that_32_bits_do_not_hold(table):
             K.kvl_attn_plan(attn, hit, app, [np.array([1, 2])], K.KVL_GATHER | K.KVL_HOST_ONLY)
         assert e.value.code == K.KVL_ERANGE
     assert K.kvl_pages_adopt(pages, [np.array([5, 2]), [6, 1]], np.array([20, 20])).size == 2      # (other types hold what is in the pool)
+
+
+@pytest.mark.parametrize("size,blocks", [((1 << 32) + 1, 1), (1 << 63, 1), (16, 1 << 31), (16, 1 << 63)])
+def test_pools_of_more_than_a_plane_takes(size, blocks):
+    layout = P.kvl_page_layout_t(1, 1, (C.c_uint64 * len(P.kvl_page_layout_t().block_bytes))(size), blocks)
+    out = C.c_void_p()
+    assert P._lib.kvl_page_pools(C.byref(layout), (C.c_void_p * 1)(4096), K.KVL_NO_POINTER_CHECKS, C.byref(out)) == K.KVL_ERANGE
+    assert not out.value
