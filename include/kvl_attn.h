@@ -168,7 +168,8 @@ int kvl_attn_layer(const kvl_attn_plan_t *plan, const kvl_attn_t *args, const vo
 /* kvl_attn_layer with other scores: in the place of s = scale * <q, K_t>
  *   cap * tanh(s / cap)  where cap is not 0,  less  slopes[H] * |p - t|  where there are slopes (H: the query head).
  * cap: 0, or from 2^-10 to 2^10 (KVL_EINVAL): a capped score is held to 2^-20 of the cap.
- * slopes: device, float [q_heads], or NULL; without a cap the scale is then from 2^-64 to 2^64 (KVL_EINVAL).  A bias and the score that it is added to
+ * slopes: device, float [q_heads], or NULL; without a cap the scale is then from 2^-64 to 2^64 (KVL_EINVAL).  A head's rows may be NaN where
+ * |slope| times the number of tokens, or 64 |slope| / scale without a cap, is beyond 2^120.  A bias and the score that it is added to
  * are rounded to 32 bits a few times: a bias is off by up to 2^-22 of what it is 64 tokens further away.
  * scores: NULL for neither. */
 typedef struct {

@@ -53,7 +53,7 @@ int kvl_pages_truncate(kvl_pages_t *pages, const uint64_t *sequences, const uint
 /* Sequences end. */
 int kvl_pages_free(kvl_pages_t *pages, const uint64_t *sequences, uint32_t n);
 /* Blocks in use move to the front of the pool: the last one in use to the first free one, until `most` have moved or no free block lies
- * before one in use.  All tables follow.  copies: host array of `most`; *n_copies: how many have moved.  No copy's source is another's destination; the copies have to be made
+ * before one in use.  All tables follow.  It looks at all blocks beyond as many as are in use, and at all tables, whatever `most` is.  copies: host array of `most`; *n_copies: how many have moved.  No copy's source is another's destination; the copies have to be made
  * before anything else is written to the pool's blocks. */
 int kvl_pages_compact(kvl_pages_t *pages, uint32_t most, kvl_block_copy_t *copies, uint32_t *n_copies);
 

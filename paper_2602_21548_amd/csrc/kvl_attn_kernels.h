@@ -179,8 +179,8 @@ __device__ __forceinline__ Seen seen_from(const AttnItem &it, const AttnBounds &
 // token t0 and the number k of a key in it.  The first part is added once, to what is taken off all of a lane's exponents.  The second is one operation with a
 // constant a score in the kernel for few rows.  In that for many it is a product of keys by rows, which the matrix unit adds: k is a bf16 number, the slope three
 // of them (24 bits; products and sums are in 32 bits as the scores' are).  Tiles in which first tokens end, or of a prefix beyond a row's position, take each
-// distance.  (Tails of 256 to 1024 tokens over 8 to 32 K keys, us: each distance 1435, one operation a score 1198, the matrix unit 1179, without a bias
-// 1020; few rows are level.)
+// distance.  (Tails of 256 to 1024 tokens over 8 to 32 K keys, us: each distance 1435, one operation a score 1198, the matrix unit 1179, of a kernel that took 1020
+// without a bias; the present one takes 1105 with and 940 without on one card, 1189 and 1015 on another.  Few rows are level.)
 struct Bias {
     float slope;
     uint32_t position;
@@ -663,10 +663,13 @@ __global__ void __launch_bounds__(256, SCORED && E4M3 && RT == 1 ? 3 : 2) kvl_at
 // its codes alone there, keys' as fp16, values' as bf16; the keys' scales multiply scores, the values' the weights, in 32 bits, and a weight is two
 // bf16 numbers, the second one what the first leaves (their products with codes are exact, and a weight keeps 16 bits).
 //
-// What bounds it is how many instructions two wavefronts a SIMD issue for a tile (the matrix unit is busy for 36 to 40 % of the time, the vector unit for 30 to 46 %, and
-// each instruction taken out of a tile's loop takes its share of the time with it): so a tile's keys and values are addressed from one register each,
-// in the LDS (rows padded, not turned: 1020 to 970 us for 16-bit tails over 8 to 32 K keys, with the next two) and in memory (32 bits from one address), and what all rows see is
-// two numbers.  870 TFLOP/s there, 950 over an 8-bit cache (by the card; the library's product of 8192^3 reaches 1207); heads of 64, 600 under a window.
+// Neither unit is full (the matrix unit is busy for 36 to 40 % of the time, the vector unit for 30 to 46 %): a wavefront does a tile's products and its softmax one
+// after the other, and the two wavefronts a SIMD that registers allow do not cover for each other.  So each instruction taken out of a tile's loop takes its share of the time with
+// it: a tile's keys and values are addressed from one register each, in the LDS (rows padded, not turned) and in memory (32 bits from one address), and what all rows see is
+// two numbers: 1020 to 970 us for 16-bit tails of 256 to 1024 tokens over 8 to 32 K keys, their join of 50 us included.  By the card such a call takes 940 to 1015 us, 830 to 900
+// TFLOP/s; over an 8-bit cache tails reach 850 to 895, whole prompts 930 (the library's product of 8192^3 1207 to 1439); heads of 64, 600 under a window.
+//
+// SCORED instances for heads of 64 do not fit the registers of three wavefronts a SIMD: 8 bytes a lane of scratch memory over a 16-bit cache, 24 in fp16 over an 8-bit one.
 template <typename T, bool E4M3>
 __device__ __forceinline__ void codes_to_half(u32x4 w, float scale, u32x4 *x, u32x4 *y) {
     uint32_t e[8];
@@ -705,8 +708,8 @@ __device__ __forceinline__ void repeat(F &&f) {
     }
 }
 
-// Loads at a number of bytes in 32 bits from one address: no arithmetic in 64, which planes of 4 GiB and more take.  (16-bit tails over 8 to 32 K keys: 1025 us
-// in 64 bits, 1000 so.)
+// Loads at a number of bytes in 32 bits from one address: no arithmetic in 64, which planes of 4 GiB and more take.  (The tails above: 1025 us in
+// 64 bits, 1000 so, in an earlier form of this kernel.)
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t near_of(const char *at) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at), 0, 0xffffffffu, 0x00020000);
 }

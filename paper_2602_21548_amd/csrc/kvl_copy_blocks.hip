@@ -26,8 +26,9 @@ constexpr uint32_t kFewCopies = 24, kMostCopies = 320;
 // 128 KB, us, apart / together: 16 layers 146 / 121, 4 layers 40 / 22, one (34 MB written) 10.9 / 7.1; but 4 MB written 2.7 / 3.3.
 constexpr uint32_t kShare = 8;
 constexpr uint64_t kShareBytes = 16u << 20;
-// Up to this many bytes the stores are sc1 ones, which the on-die cache takes, beyond it sc1+nt ones (as a move's): 57 MB 17.3 / 21.2 us, 134 MB of
-// eight ways on 21.7 / 27.8, 513 MB 191 / 170.
+// Up to this many bytes the stores are sc1 ones, which the on-die cache takes, beyond it sc1+nt ones (as a move's).  us, sc1 / sc1+nt, 64 KB blocks of 16 layers: 67 MB
+// 20 / 22, 134 MB 39.5 / 45.6, 255 MB 73 / 84, 319 MB 95.5 / 103.5, 401 MB 132 / 133, 512 MB 172 / 168, 1006 MB 337 / 328; eight ways on from each block 134 MB 20.7 / 25.7, 255 MB
+// 40 / 53, 401 MB 78 / 86.5, 512 MB 110.5 / 113.6, 671 MB 150 / 150: level at 400 MB, or 670; the limit is the size of that cache.
 constexpr uint64_t kCachedCopyBytes = 256u << 20;
 
 struct CopyPlane {
