@@ -111,7 +111,7 @@ static int attn_layer(const kvl_attn_plan_t *plan, const kvl_attn_t *in, const k
     a.slopes = how.slopes;
     if (plan->masked) a.bounds = reinterpret_cast<const AttnBounds *>(reinterpret_cast<const char *>(plan->base.d_units) + plan->off_bounds);
     AttnLaunch go(plan, stream);
-    if (a.cap != 0 || a.slopes || a.bounds) launch_types<true>(plan, a, go);
+    if (a.cap != 0 || a.slopes || a.bounds || (codes && a.c > kMostFactor)) launch_types<true>(plan, a, go);
     else launch_types<false>(plan, a, go);
     return go.made();
 }

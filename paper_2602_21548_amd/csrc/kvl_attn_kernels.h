@@ -47,6 +47,9 @@ struct ScoredArgs : AttnArgs {
     float cap;                          // cap * log2(e); 0: none
     float over;                         // 1 / (2 cap), without a cap 1 / c
 };
+// Up to this factor of scores (c) floats hold it times a block's scale (at most 2^63).  What it is beyond that comes apart over an 8-bit cache, so that a product of 0 stays 0: in
+// the SCORED kernels, which take such factors without other scores, too.
+constexpr float kMostFactor = 0x1p64f;
 template <bool SCORED>
 using ArgsOf = std::conditional_t<SCORED, ScoredArgs, AttnArgs>;
 
@@ -433,8 +436,7 @@ __global__ void __launch_bounds__(256, SCORED && E4M3 && RT == 1 ? 3 : 2) kvl_at
         if (E4M3) {
             if (lane < KT) {
                 const float by = in_range(scales.v);
-                // (held to what floats hold: a product of 0 is a score of 0, whatever it is multiplied by)
-                key_c[lane] = fminf(a.c * in_range(scales.k), 3.40282347e38f);
+                key_c[lane] = (SCORED ? fminf(a.c, kMostFactor) : a.c) * in_range(scales.k);
                 key_log[lane] = __log2f(by);
                 key_over[lane] = __builtin_amdgcn_rcpf(by);        // (to a unit in the last place of 32 bits, as the sum it goes into)
             }
@@ -478,6 +480,12 @@ __global__ void __launch_bounds__(256, SCORED && E4M3 && RT == 1 ? 3 : 2) kvl_at
 #pragma unroll
                     for (int r = 0; r < R; ++r) s[r][b] = T::mma16(k, x[r], s[r][b]);
                 }
+            }
+            if (SCORED && E4M3 && a.c > kMostFactor) {
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) s[r][b] *= a.c / kMostFactor;
             }
             TV8 p[R][NB / 2], p_rest[R][NB / 2];
 #pragma unroll

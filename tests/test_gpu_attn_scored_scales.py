@@ -42,6 +42,22 @@ def test_zero_products_under_factors_beyond_floats(hit, app, heads, dim, dtype, 
     close(b, *attend(b), (w_out, w_lse, weight, 0 * reach))
 
 
+@pytest.mark.parametrize("hit,app,heads", ROWS)
+@pytest.mark.parametrize("dim", [64, 128])
+def test_scores_that_floats_hold_of_factors_that_they_do_not(hit, app, heads, dim):
+    """Queries of 2^-120 over codes of 1/16 to 5/32 with scales of 2^62 and 2^63, times 2^66: scores of 32 to 40, of which a factor held to the largest float makes others."""
+    b = Scored(hit, app, 16, heads, dim, torch.bfloat16, True, seed=4)
+    b.scale = 2.0 ** 66
+    low = b.g.random(b.scales[0].shape) < 0.5
+    b.scales[0] = np.where(np.isnan(b.scales[0]), np.nan, np.where(low, 2.0 ** 62, 2.0 ** 63)).astype(np.float32)
+    b.q.zero_()
+    b.q[..., 5] = 2.0 ** -120
+    # (codes of 1/16 times 1, 9/8, 10/8; twice that under the lower scale)
+    codes = 0x18 + b.g.integers(0, 3, size=b.pools[0].shape[:3]) + 8 * low[:, None, :]
+    b.pools[0][..., 5] = np.where(b.held[..., None], codes, 0x7F)
+    close(b, *attend(b), b.want())
+
+
 # Every block of K, of V or of both out of fp16's range, and scales between powers of two --------------------------------------------------
 
 def other(b, cap, slopes, prefix, documents):
